@@ -15,9 +15,9 @@ public binding:
 
 With `own` false, `run` computes the same in elementary torch operations in 32
 bits.  A matrix held with block scales is its codes [rows, pitch] (two E2M1 codes
-a byte, the even column in the low half) and its scales [groups, rows, 8]: a
+a byte, the even column in the low half) and its scales [groups, slots, 8]: a
 group is 256 columns, one byte 2^(s - 127) for each 32 of them; columns are
-filled up to whole groups with zeros.
+filled up to whole groups with zeros, the scales' rows up to a multiple of 32.
 """
 import math
 
@@ -119,7 +119,7 @@ def _held(x, fmt):
     groups = -(-cols // GROUP)
     per = 2 if fmt == "fp4" else 1
     codes = torch.empty(rows, groups * GROUP // per, dtype=torch.uint8, device=x.device)
-    scales = torch.empty(groups, rows, 8, dtype=torch.uint8, device=x.device)
+    scales = torch.zeros(groups, rows + -rows % 32, 8, dtype=torch.uint8, device=x.device)
     for r in range(0, rows, 16384):
         part = torch.nn.functional.pad(x[r:r + 16384], (0, groups * GROUP - cols))
         v, s = _scaled(part, fmt)
@@ -133,7 +133,7 @@ def _held(x, fmt):
             codes[r:r + 16384] = code[:, 0::2] + 16 * code[:, 1::2]
         else:
             codes[r:r + 16384] = v.to(torch.float8_e4m3fn).view(torch.uint8)
-        scales[:, r:r + 16384] = s.view(-1, groups, 8).permute(1, 0, 2)
+        scales[:, r:r + len(part)] = s.view(-1, groups, 8).permute(1, 0, 2)
     return codes, scales
 
 
@@ -264,7 +264,7 @@ def _decode(codes, scales, fmt, cols):
     else:
         v = codes.view(torch.float8_e4m3fn).float()
     rows = codes.shape[0]
-    s = scales.permute(1, 0, 2).reshape(rows, -1, 1).int() - 127
+    s = scales[:, :rows].permute(1, 0, 2).reshape(rows, -1, 1).int() - 127
     return torch.ldexp(v.view(rows, -1, 32), s).view(rows, -1)[:, :cols].contiguous()
 
 
@@ -355,7 +355,8 @@ def exact(case, seed):
             man = man.double() / 2 ** digits
             v = torch.where(ex == 0, man * 2.0 ** (1 - bias), (1 + man) * 2.0 ** (ex - bias).double())
             v = v * (1 - 2 * sign.double())
-            s = 2.0 ** (scales.permute(1, 0, 2).reshape(c.shape[0], -1).double() - 127)
+            s = scales[:, :len(c)].permute(1, 0, 2).reshape(len(c), -1)
+            s = 2.0 ** (s.double() - 127)
             return (v.view(c.shape[0], -1, 32) * s[:, :, None]).view(c.shape[0], -1)[:, :case["K"]]
         a = of(st["a"], case["fmt"])
         codes, scales = st["b"]
