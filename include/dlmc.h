@@ -337,6 +337,85 @@ dlmc_status dlmc_rank_rows(dlmc_model* model, const float* logits, int32_t n_row
                            const int32_t* sym, int32_t* rank);
 dlmc_status dlmc_select_rank_rows(dlmc_model* model, const float* logits, int32_t n_rows,
                                   const int32_t* rank, int32_t* sym);
+/* ---- block-scaled values and token scores (device pointers) -------------- */
+
+/* The calls of this section enqueue their work on the model's stream and return
+ * without waiting for it: results are ready once the stream has come that far.
+ * They allocate nothing and keep no state between calls, so they may be captured
+ * into a HIP graph (once the model's stream is the capturing one), and calls on
+ * several streams do not disturb each other.  They leave the calling thread's
+ * current device as it was.  Element types are DLMC_DTYPE_F32 and
+ * DLMC_DTYPE_BF16; ld* is the distance of two rows in elements (>= the row's
+ * length) and rows need no alignment beyond their elements' own (rows of whole
+ * 16-byte chunks are faster). */
+
+/* Values with block scales: blocks of 32 consecutive columns of a row share a
+ * scale 2^(s - 127), one byte, 255 for NaN; the values are E2M1 (+-0, 0.5, 1, 1.5,
+ * 2, 3, 4, 6) or E4M3 (largest 448).  A matrix [rows, cols] is held in two device
+ * arrays, 16-byte aligned, of dlmc_mx_bytes bytes:
+ *   codes [rows, pitch]: cols rounded up to a multiple of 256, E4M3 one byte a
+ *     column, E2M1 two columns a byte, the even one in the low half; the columns
+ *     past cols are zero
+ *   scales [groups, slots, 8]: groups of 256 columns, slots = rows rounded up to a
+ *     multiple of 32, one byte for each of a group's eight blocks (slots past rows
+ *     may hold anything)
+ * 1 <= cols <= 2^24. */
+#define DLMC_MX_FP4 0 /* E2M1 */
+#define DLMC_MX_FP8 1 /* E4M3 */
+/* Bytes of the two arrays (host only, no GPU needed). */
+dlmc_status dlmc_mx_bytes(int32_t fmt, int32_t rows, int32_t cols, uint64_t* code_bytes,
+                          uint64_t* scale_bytes);
+/* Quantise x[rows, cols] of `dtype`.  A block's scale is the least power of two
+ * 2^e, e >= -127, whose multiple by the format's largest value is no less than the
+ * block's largest magnitude, so that nothing saturates; each value goes to the
+ * nearest code, ties to even.  A block that holds a NaN or an infinity gets the
+ * scale NaN. */
+dlmc_status dlmc_mx_quantize(dlmc_model* model, const void* x, int32_t dtype, int64_t ldx,
+                             int32_t rows, int32_t cols, int32_t fmt, uint8_t* codes,
+                             uint8_t* scales);
+/* The values held, in `dtype` (exact in fp32; in bf16 too, down to its least
+ * normal value). */
+dlmc_status dlmc_mx_dequantize(dlmc_model* model, const uint8_t* codes, const uint8_t* scales,
+                               int32_t fmt, int32_t rows, int32_t cols, void* out, int32_t dtype,
+                               int64_t ldo);
+/* Pre-norm of a residual stream with its branch's addition: r = x + delta (x
+ * alone if delta is NULL), rounded to x's type and stored in sum[rows, cols] (of
+ * x's type; may be x itself; NULL: not stored; x, delta and sum must not overlap
+ * otherwise), then y = r / sqrt(mean(r^2) + eps) (DLMC_NORM_RMS) or (r - mean(r)) /
+ * sqrt(var(r) + eps) (DLMC_NORM_LAYER), times gain[cols] (fp32; NULL: 1),
+ * quantised as by dlmc_mx_quantize.  All arithmetic is in fp32; a row's result
+ * does not depend on the others.  cols <= 8192. */
+dlmc_status dlmc_add_norm_mx(dlmc_model* model, const void* x, int32_t dtype, int64_t ldx,
+                             const void* delta, int32_t delta_dtype, int64_t ldd, void* sum,
+                             int64_t lds, const float* gain, int32_t norm_kind, float eps,
+                             int32_t rows, int32_t cols, int32_t fmt, uint8_t* codes,
+                             uint8_t* scales);
+/* out[M, N] = A B^T of A [M, K] held in fmt_a and B [N, K] held in E2M1,
+ * accumulated in fp32, in out_dtype.  A row's result does not depend on the other
+ * rows or their number.  The products of E2M1 values are summed exactly within 64
+ * columns; with E4M3 the matrix unit drops what lies 2^13 below the largest of the
+ * products that it adds together. */
+dlmc_status dlmc_mx_matmul(dlmc_model* model, const uint8_t* a_codes, const uint8_t* a_scales,
+                           int32_t fmt_a, const uint8_t* b_codes, const uint8_t* b_scales,
+                           int32_t M, int32_t N, int32_t K, void* out, int32_t out_dtype,
+                           int64_t ldo);
+/* Scores of device logit rows [n_rows, vocab] of `dtype`, ld apart, in one pass:
+ * logp_bits[i] = log2 of the probability of tokens[i] in row i (its negative is the
+ * ideal code length in bits; tokens and logp_bits may both be NULL; a token of -1
+ * stands for none and gives 0, another outside [0, vocab) NaN), entropy_bits[i],
+ * and the n_top (0..64, <= vocab) most probable symbols in descending order, equal
+ * logits by token id, as for dlmc_rank_rows: top_ids and top_logp_bits [n_rows,
+ * n_top] (may be NULL if n_top is 0).  A logit of -inf rules a symbol out
+ * (log2 p = -inf).  A row without a distribution -- nothing above -inf, a NaN, or an
+ * infinity -- gives NaN, and ids of -1.  ws: dlmc_token_scores_ws bytes of device
+ * memory, 16-byte aligned, for this call alone (may be NULL if that is 0). */
+dlmc_status dlmc_token_scores(dlmc_model* model, const void* logits, int32_t dtype, int64_t ld,
+                              int32_t n_rows, const int32_t* tokens, int32_t n_top,
+                              float* logp_bits, float* entropy_bits, int32_t* top_ids,
+                              float* top_logp_bits, void* ws, uint64_t ws_bytes);
+dlmc_status dlmc_token_scores_ws(const dlmc_model* model, int32_t n_rows, int32_t n_top,
+                                 uint64_t* ws_bytes);
+
 /* Attention-based context scores of one chunk of host tokens[0..T) into
  * host scores[0..T) (two extra forward passes, T <= max_chunk). */
 dlmc_status dlmc_context_scores(dlmc_model* model, const int32_t* tokens, int32_t T, float* scores);

@@ -10,6 +10,7 @@ streams to the stage hooks.
 from __future__ import annotations
 
 import ctypes
+import dataclasses
 import os
 import re
 from typing import Callable, Optional, Sequence
@@ -23,6 +24,7 @@ HEADER = os.path.join(os.path.dirname(HERE), "include", "dlmc.h")
 FFN = {"gelu": 0, "swiglu": 1}
 NORM = {"layernorm": 0, "rmsnorm": 1}
 DTYPE = {"f32": 0, "bf16": 1}
+MX_FORMAT = {"fp4": 0, "fp8": 1}  # E2M1, E4M3
 FLAG_CRC = 1
 STAGES = ["embed", "norm", "qkv", "attn", "oproj", "ffn_in", "ffn_out", "head", "entropy",
           "select", "cdf", "reveal", "compact"]
@@ -79,6 +81,7 @@ TRACE_FN = ctypes.CFUNCTYPE(None, ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint
 _lib = None
 P = ctypes.POINTER
 vp, i32, u32, u64, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint32, ctypes.c_uint64, ctypes.c_float
+i64 = ctypes.c_int64
 _SIGS = {
     "dlmc_model_create": (i32, [P(ModelConfig), u64, i32, P(vp)]),
     "dlmc_model_destroy": (None, [vp]),
@@ -114,6 +117,14 @@ _SIGS = {
     "dlmc_test_head_logits": (i32, [vp, i32]),
     "dlmc_test_gemm_tiles": (i32, [i32, i32, i32, i32, i32, ctypes.POINTER(ctypes.c_int32),
                                    ctypes.POINTER(ctypes.c_int32)]),
+    "dlmc_mx_bytes": (i32, [i32, i32, i32, P(u64), P(u64)]),
+    "dlmc_mx_quantize": (i32, [vp, vp, i32, i64, i32, i32, i32, vp, vp]),
+    "dlmc_mx_dequantize": (i32, [vp, vp, vp, i32, i32, i32, vp, i32, i64]),
+    "dlmc_add_norm_mx": (i32, [vp, vp, i32, i64, vp, i32, i64, vp, i64, vp, i32, f32, i32, i32, i32,
+                               vp, vp]),
+    "dlmc_mx_matmul": (i32, [vp, vp, vp, i32, vp, vp, i32, i32, i32, vp, i32, i64]),
+    "dlmc_token_scores": (i32, [vp, vp, i32, i64, i32, vp, i32, vp, vp, vp, vp, vp, u64]),
+    "dlmc_token_scores_ws": (i32, [vp, i32, i32, P(u64)]),
     "dlmc_status_string": (ctypes.c_char_p, [i32]),
     "dlmc_last_error": (ctypes.c_char_p, []),
 }
@@ -153,6 +164,30 @@ def _ptr(a) -> int:
     if isinstance(a, np.ndarray):
         return a.ctypes.data
     return a.data_ptr()
+
+
+def _refuse(why: str):
+    raise DlmcError(-1, lib().dlmc_status_string(-1).decode(), why)
+
+
+@dataclasses.dataclass
+class MXMatrix:
+    """A matrix [rows, cols] held with block scales (include/dlmc.h gives the
+    layout): torch uint8 tensors codes [rows, pitch] and scales [groups, slots, 8]
+    on the GPU; fmt "fp4" (E2M1) or "fp8" (E4M3)."""
+    codes: object
+    scales: object
+    fmt: str
+    rows: int
+    cols: int
+
+    @staticmethod
+    def empty(fmt: str, rows: int, cols: int, device) -> "MXMatrix":
+        import torch
+        groups = -(-cols // 256)
+        codes = torch.empty((rows, groups * (128 if fmt == "fp4" else 256)), dtype=torch.uint8, device=device)
+        scales = torch.empty((groups, -(-rows // 32) * 32, 8), dtype=torch.uint8, device=device)
+        return MXMatrix(codes, scales, fmt, rows, cols)
 
 
 def model_config(shape, max_chunk: int, max_batch: int) -> ModelConfig:
@@ -224,6 +259,7 @@ class Model:
         h = vp()
         _check(lib().dlmc_model_create(ctypes.byref(self.cfg), shape.seed, device, ctypes.byref(h)))
         self.handle = h
+        self.device = device
         self._trace_cb = None
         self._stream = None  # what set_stream was last given
         self._hook_stream = False  # whether that was a stage hook's default stream
@@ -456,6 +492,155 @@ class Model:
                                 int(rows.numel()), B, T, tau, m_min, m_max, sel_pos, sel_row,
                                 n_sel)
         return sel_pos, sel_row, n_sel
+
+    # ---- block-scaled values and token scores (torch device tensors; the calls
+    # return without waiting for the GPU)
+    def _rows(self, t, what: str, cols: Optional[int] = None):
+        """(DTYPE code, row distance) of a 2-d fp32 or bf16 tensor on this GPU whose
+        rows are contiguous; `cols` if it has to have that many columns."""
+        import torch
+        if not torch.is_tensor(t) or t.dim() != 2:
+            _refuse(f"{what} must be a 2-d tensor")
+        code = 0 if t.dtype == torch.float32 else 1 if t.dtype == torch.bfloat16 else _refuse(
+            f"{what} must be float32 or bfloat16, not {t.dtype}")
+        self._here(t, what)
+        if cols is not None and t.shape[1] != cols:
+            _refuse(f"{what} must have {cols} columns, not {t.shape[1]}")
+        if t.shape[1] > 1 and t.stride(1) != 1:
+            _refuse(f"{what} must have contiguous rows")
+        if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+            _refuse(f"{what}: rows overlap")
+        return code, t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+    def _here(self, t, what: str):
+        if t.device.type != "cuda" or t.device.index != self.device:
+            _refuse(f"{what} must be on the model's GPU (cuda:{self.device}), not on {t.device}")
+
+    def _vector(self, t, what: str, n: int, dtype):
+        import torch
+        if not torch.is_tensor(t) or t.dtype != dtype or t.dim() != 1 or t.shape[0] != n:
+            _refuse(f"{what} must be a tensor of {n} {dtype} values")
+        self._here(t, what)
+        return t.contiguous()
+
+    def _held(self, q, what: str, fmt: Optional[str] = None):
+        if not isinstance(q, MXMatrix) or q.fmt not in MX_FORMAT or q.rows < 0 or not 1 <= q.cols <= 1 << 24:
+            _refuse(f"{what} must be an MXMatrix")
+        if fmt is not None and q.fmt != fmt:
+            _refuse(f"{what} must be held in {fmt}, not in {q.fmt}")
+        groups = -(-q.cols // 256)
+        for t, shape in ((q.codes, (q.rows, groups * (128 if q.fmt == "fp4" else 256))),
+                         (q.scales, (groups, -(-q.rows // 32) * 32, 8))):
+            if tuple(t.shape) != shape or not t.is_contiguous() or t.element_size() != 1:
+                _refuse(f"{what}: codes or scales do not fit {q.rows} x {q.cols} in {q.fmt}")
+            self._here(t, what)
+
+    @staticmethod
+    def _format(fmt: str) -> int:
+        return MX_FORMAT[fmt] if fmt in MX_FORMAT else _refuse(f"format must be fp4 or fp8, not {fmt!r}")
+
+    @staticmethod
+    def _out_type(dtype) -> int:
+        import torch
+        return 0 if dtype == torch.float32 else 1 if dtype == torch.bfloat16 else _refuse(
+            f"output type must be float32 or bfloat16, not {dtype}")
+
+    def mx_quantize(self, x, fmt: str = "fp4") -> MXMatrix:
+        """x [rows, cols] (fp32 or bf16) in E2M1 ("fp4") or E4M3 ("fp8") with a
+        power-of-two scale for each 32 columns; nothing saturates."""
+        code, ld = self._rows(x, "x")
+        f = self._format(fmt)
+        q = MXMatrix.empty(fmt, x.shape[0], x.shape[1], x.device)
+        self._on_current_stream(x.device, lib().dlmc_mx_quantize, x, code, ld, q.rows, q.cols, f, q.codes, q.scales)
+        return q
+
+    def mx_dequantize(self, q: MXMatrix, dtype=None):
+        """The values that q holds, bf16 (the default: exact) or fp32 [rows, cols]."""
+        import torch
+        dtype = torch.bfloat16 if dtype is None else dtype
+        code = self._out_type(dtype)
+        self._held(q, "q")
+        out = torch.empty((q.rows, q.cols), dtype=dtype, device=q.codes.device)
+        self._on_current_stream(out.device, lib().dlmc_mx_dequantize, q.codes, q.scales, MX_FORMAT[q.fmt], q.rows,
+                                q.cols, out, code, q.cols)
+        return out
+
+    def add_norm_mx(self, x, delta=None, gain=None, fmt: str = "fp8", norm: Optional[str] = None,
+                    eps: Optional[float] = None, out=None):
+        """(r, q): r = x + delta [rows, cols] in x's type (x itself without a delta;
+        written to `out`, which may be x, if given) and its norm times gain (fp32)
+        as an MXMatrix.  norm ("rmsnorm" or "layernorm") and eps: the model's."""
+        import torch
+        code, ld = self._rows(x, "x")
+        rows, cols = x.shape
+        kind = self.shape.norm if norm is None else norm
+        if kind not in NORM:
+            _refuse(f"norm must be rmsnorm or layernorm, not {kind!r}")
+        dcode, ldd = self._rows(delta, "delta", cols) if delta is not None else (0, 0)
+        if delta is not None and delta.shape[0] != rows:
+            _refuse(f"delta must have {rows} rows, not {delta.shape[0]}")
+        f = self._format(fmt)
+        if gain is not None:
+            gain = self._vector(gain, "gain", cols, torch.float32)
+        if out is None:
+            r = x if delta is None else torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+            total = None if delta is None else r
+        else:
+            r = total = out
+        lds = 0
+        if total is not None:
+            ocode, lds = self._rows(total, "out", cols)
+            if ocode != code or total.shape[0] != rows:
+                _refuse("out must have x's shape and type")
+        q = MXMatrix.empty(fmt, rows, cols, x.device)
+        self._on_current_stream(x.device, lib().dlmc_add_norm_mx, x, code, ld, delta, dcode, ldd, total, lds, gain,
+                                NORM[kind], self.shape.norm_eps if eps is None else eps, rows, cols, f, q.codes,
+                                q.scales)
+        return r, q
+
+    def mx_matmul(self, a: MXMatrix, b: MXMatrix, out_dtype=None, out=None):
+        """a b^T [a.rows, b.rows] of a in either format and b in E2M1, accumulated in
+        fp32, as fp32 (the default) or bf16, into `out` if given."""
+        import torch
+        self._held(a, "a")
+        self._held(b, "b", "fp4")
+        if a.cols != b.cols:
+            _refuse(f"a has {a.cols} columns, b {b.cols}")
+        if out is None:
+            dtype = torch.float32 if out_dtype is None else out_dtype
+            code, ldo = self._out_type(dtype), b.rows
+            out = torch.empty((a.rows, b.rows), dtype=dtype, device=a.codes.device)
+        else:
+            code, ldo = self._rows(out, "out", b.rows)
+            if out.shape[0] != a.rows or (out_dtype is not None and out.dtype != out_dtype):
+                _refuse("out does not have the product's shape and type")
+        self._on_current_stream(out.device, lib().dlmc_mx_matmul, a.codes, a.scales, MX_FORMAT[a.fmt], b.codes,
+                                b.scales, a.rows, b.rows, a.cols, out, code, ldo)
+        return out
+
+    def token_scores(self, logits, tokens=None, top: int = 0):
+        """Of logits [n, vocab] (fp32 or bf16): (log2 probability of tokens[i] in row
+        i (None without tokens), entropy in bits, ids [n, top] of the most probable
+        symbols, their log2 probabilities)."""
+        import torch
+        V = self.shape.vocab
+        code, ld = self._rows(logits, "logits", V)
+        n, dev = logits.shape[0], logits.device
+        if not 0 <= top <= min(64, V):
+            _refuse("top must be in 0..64, at most the vocabulary")
+        logp = None
+        if tokens is not None:
+            tokens = self._vector(tokens, "tokens", n, torch.int32)
+            logp = torch.empty(n, dtype=torch.float32, device=dev)
+        H = torch.empty(n, dtype=torch.float32, device=dev)
+        ids = torch.empty((n, top), dtype=torch.int32, device=dev)
+        tlp = torch.empty((n, top), dtype=torch.float32, device=dev)
+        need = u64(0)
+        _check(lib().dlmc_token_scores_ws(self.handle, n, top, ctypes.byref(need)))
+        ws = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
+        self._on_current_stream(dev, lib().dlmc_token_scores, logits, code, ld, n, tokens, top, logp, H, ids, tlp,
+                                ws, need.value)
+        return logp, H, ids, tlp
 
     def weight(self, tensor_id: int, rows: int, cols: int) -> np.ndarray:
         """A weight tensor in canonical [out, in] layout (uint16 bf16 bits or float32)."""

@@ -1,5 +1,6 @@
 // extern "C" entry points of libdlmc.so: argument checks, exception to
 // status conversion, thread-local error text.
+#include <cmath>
 #include <cstring>
 #include <new>
 #include <string>
@@ -38,6 +39,45 @@ dlmc_status guard(F&& f) {
 void use(dlmc_model* m) {
   DLMC_CHECK(m, DLMC_E_INVAL, "model is NULL");
   DLMC_HIP(hipSetDevice(m->device));
+}
+
+// The model's device for the length of a call that returns without waiting; the
+// caller's device is current again afterwards.
+struct OnDevice {
+  int before = -1;
+  explicit OnDevice(const dlmc_model* m) {
+    DLMC_CHECK(m, DLMC_E_INVAL, "model is NULL");
+    DLMC_HIP(hipGetDevice(&before));
+    if (before == m->device)
+      before = -1;
+    else
+      DLMC_HIP(hipSetDevice(m->device));
+  }
+  ~OnDevice() {
+    if (before >= 0) (void)hipSetDevice(before);
+  }
+};
+
+bool is_bf16(int32_t dtype) {
+  DLMC_CHECK(dtype == DLMC_DTYPE_F32 || dtype == DLMC_DTYPE_BF16, DLMC_E_INVAL, "element type must be fp32 or bf16");
+  return dtype == DLMC_DTYPE_BF16;
+}
+// rows of n elements, ld apart, of `bytes`-byte elements
+void check_rows(const void* p, int64_t ld, int32_t n, int bytes, const char* what) {
+  DLMC_CHECK(p, DLMC_E_INVAL, std::string(what) + " is NULL");
+  DLMC_CHECK((uintptr_t)p % bytes == 0, DLMC_E_INVAL, std::string(what) + " is not aligned to its elements");
+  DLMC_CHECK(ld >= n, DLMC_E_INVAL, std::string(what) + ": rows overlap");
+}
+void check_mx_shape(int32_t fmt, int32_t rows, int32_t cols) {
+  DLMC_CHECK(fmt == DLMC_MX_FP4 || fmt == DLMC_MX_FP8, DLMC_E_INVAL, "no such block-scaled format");
+  DLMC_CHECK(rows >= 0, DLMC_E_INVAL, "negative number of rows");
+  DLMC_CHECK(cols >= 1 && cols <= (1 << 24), DLMC_E_INVAL, "columns must be in 1..2^24");
+}
+MxView mx_view(const uint8_t* codes, const uint8_t* scales) {
+  DLMC_CHECK(codes && scales, DLMC_E_INVAL, "codes or scales are NULL");
+  DLMC_CHECK((((uintptr_t)codes | (uintptr_t)scales) & 15) == 0, DLMC_E_INVAL,
+             "codes and scales must be 16-byte aligned");
+  return MxView{const_cast<uint8_t*>(codes), const_cast<uint8_t*>(scales)};
 }
 
 dlmc_status write_out(const std::vector<uint8_t>& bytes, uint8_t* out, uint64_t cap,
@@ -393,6 +433,123 @@ dlmc_status dlmc_profile_read(dlmc_model* m, int32_t stage, double* ms_total, ui
     if (ms_total) *ms_total = m->prof_ms[stage];
     if (launches) *launches = m->prof_n[stage];
     if (work) *work = m->prof_work[stage];
+  });
+}
+
+dlmc_status dlmc_mx_bytes(int32_t fmt, int32_t rows, int32_t cols, uint64_t* code_bytes, uint64_t* scale_bytes) {
+  return guard([&] {
+    check_mx_shape(fmt, rows, cols);
+    DLMC_CHECK(code_bytes && scale_bytes, DLMC_E_INVAL, "NULL argument");
+    *code_bytes = mx_code_bytes(fmt, rows, cols);
+    *scale_bytes = mx_scale_bytes(rows, cols);
+  });
+}
+
+dlmc_status dlmc_mx_quantize(dlmc_model* m, const void* x, int32_t dtype, int64_t ldx, int32_t rows, int32_t cols,
+                             int32_t fmt, uint8_t* codes, uint8_t* scales) {
+  return guard([&] {
+    OnDevice on(m);
+    const bool bf16 = is_bf16(dtype);
+    check_mx_shape(fmt, rows, cols);
+    if (rows == 0) return;
+    check_rows(x, ldx, cols, bf16 ? 2 : 4, "x");
+    mx_quantize(m->stream, x, bf16, (size_t)ldx, rows, cols, fmt, mx_view(codes, scales));
+  });
+}
+
+dlmc_status dlmc_mx_dequantize(dlmc_model* m, const uint8_t* codes, const uint8_t* scales, int32_t fmt, int32_t rows,
+                               int32_t cols, void* out, int32_t dtype, int64_t ldo) {
+  return guard([&] {
+    OnDevice on(m);
+    const bool bf16 = is_bf16(dtype);
+    check_mx_shape(fmt, rows, cols);
+    if (rows == 0) return;
+    check_rows(out, ldo, cols, bf16 ? 2 : 4, "out");
+    mx_dequantize(m->stream, mx_view(codes, scales), fmt, rows, cols, out, bf16, (size_t)ldo);
+  });
+}
+
+dlmc_status dlmc_add_norm_mx(dlmc_model* m, const void* x, int32_t dtype, int64_t ldx, const void* delta,
+                             int32_t delta_dtype, int64_t ldd, void* sum, int64_t lds, const float* gain,
+                             int32_t norm_kind, float eps, int32_t rows, int32_t cols, int32_t fmt, uint8_t* codes,
+                             uint8_t* scales) {
+  return guard([&] {
+    OnDevice on(m);
+    AddNormMx a;
+    a.x_bf16 = is_bf16(dtype);
+    check_mx_shape(fmt, rows, cols);
+    DLMC_CHECK(cols <= ADD_NORM_MAX_COLS, DLMC_E_INVAL, "a norm takes at most 8192 columns");
+    DLMC_CHECK(norm_kind == DLMC_NORM_LAYER || norm_kind == DLMC_NORM_RMS, DLMC_E_INVAL, "norm_kind");
+    DLMC_CHECK(std::isfinite(eps) && eps >= 0.0f, DLMC_E_INVAL, "eps must be finite and not negative");
+    if (delta) a.delta_bf16 = is_bf16(delta_dtype);
+    if (rows == 0) return;
+    const int es = a.x_bf16 ? 2 : 4;
+    check_rows(x, ldx, cols, es, "x");
+    if (delta) check_rows(delta, ldd, cols, a.delta_bf16 ? 2 : 4, "delta");
+    if (sum) check_rows(sum, lds, cols, es, "sum");
+    DLMC_CHECK(sum != x || lds == ldx, DLMC_E_INVAL, "a sum stored in x has x's rows");
+    DLMC_CHECK((uintptr_t)gain % 4 == 0, DLMC_E_INVAL, "gain is not aligned to its elements");
+    a.q = mx_view(codes, scales);
+    a.x = x;
+    a.delta = delta;
+    a.sum = sum;
+    a.gain = gain;
+    a.ldx = (size_t)ldx;
+    a.ldd = (size_t)ldd;
+    a.lds = (size_t)lds;
+    a.slots = mx_slots(rows);
+    a.rows = rows;
+    a.cols = cols;
+    a.norm_kind = norm_kind;
+    a.fmt = fmt;
+    a.eps = eps;
+    add_norm_mx(m->stream, a);
+  });
+}
+
+dlmc_status dlmc_mx_matmul(dlmc_model* m, const uint8_t* a_codes, const uint8_t* a_scales, int32_t fmt_a,
+                           const uint8_t* b_codes, const uint8_t* b_scales, int32_t M, int32_t N, int32_t K,
+                           void* out, int32_t out_dtype, int64_t ldo) {
+  return guard([&] {
+    OnDevice on(m);
+    const bool bf16 = is_bf16(out_dtype);
+    check_mx_shape(fmt_a, M, K);
+    DLMC_CHECK(N >= 0, DLMC_E_INVAL, "negative number of rows");
+    if (M == 0 || N == 0) return;
+    const MxView a = mx_view(a_codes, a_scales), b = mx_view(b_codes, b_scales);
+    check_rows(out, ldo, N, bf16 ? 2 : 4, "out");
+    mx_matmul(m->stream, a, fmt_a, mx_slots(M), b, M, N, K, nullptr, out, bf16, (size_t)ldo);
+  });
+}
+
+dlmc_status dlmc_token_scores_ws(const dlmc_model* m, int32_t n_rows, int32_t n_top, uint64_t* ws_bytes) {
+  return guard([&] {
+    DLMC_CHECK(m && ws_bytes, DLMC_E_INVAL, "NULL argument");
+    DLMC_CHECK(n_rows >= 0, DLMC_E_INVAL, "negative number of rows");
+    DLMC_CHECK(n_top >= 0 && n_top <= 64 && n_top <= m->cfg.vocab, DLMC_E_INVAL, "n_top must be in 0..64, at most vocab");
+    *ws_bytes = token_scores_ws(n_rows, m->cfg.vocab, n_top);
+  });
+}
+
+dlmc_status dlmc_token_scores(dlmc_model* m, const void* logits, int32_t dtype, int64_t ld, int32_t n_rows,
+                              const int32_t* tokens, int32_t n_top, float* logp_bits, float* entropy_bits,
+                              int32_t* top_ids, float* top_logp_bits, void* ws, uint64_t ws_bytes) {
+  return guard([&] {
+    OnDevice on(m);
+    const bool bf16 = is_bf16(dtype);
+    const int V = m->cfg.vocab;
+    DLMC_CHECK(n_rows >= 0, DLMC_E_INVAL, "negative number of rows");
+    DLMC_CHECK(n_top >= 0 && n_top <= 64 && n_top <= V, DLMC_E_INVAL, "n_top must be in 0..64, at most vocab");
+    DLMC_CHECK(!tokens == !logp_bits, DLMC_E_INVAL, "tokens and logp_bits go together");
+    if (n_rows == 0) return;
+    check_rows(logits, ld, V, bf16 ? 2 : 4, "logits");
+    DLMC_CHECK(entropy_bits, DLMC_E_INVAL, "entropy_bits is NULL");
+    DLMC_CHECK(n_top == 0 || (top_ids && top_logp_bits), DLMC_E_INVAL, "no room for the alternatives");
+    const uint64_t need = token_scores_ws(n_rows, V, n_top);
+    DLMC_CHECK(need == 0 || (ws && ((uintptr_t)ws & 15) == 0 && ws_bytes >= need), DLMC_E_INVAL,
+               "the workspace needs " + std::to_string(need) + " bytes, 16-byte aligned");
+    token_scores(m->stream, logits, bf16, (size_t)ld, n_rows, V, tokens, n_top, logp_bits, entropy_bits, top_ids,
+                 top_logp_bits, ws);
   });
 }
 

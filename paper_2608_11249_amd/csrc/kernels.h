@@ -2,6 +2,7 @@
 #pragma once
 
 #include "common.h"
+#include "mx.h"
 
 namespace dlmc {
 
@@ -202,5 +203,42 @@ void rank_symbols(hipStream_t st, const float* logits, const int32_t* sel_row,
 void select_by_rank(hipStream_t st, const float* logits, const int32_t* sel_row,
                     const int32_t* sel_pos, const int32_t* n_sel, const int32_t* rank, int32_t* sym,
                     int32_t* state, int B, int T, int m_max, int V, int32_t* err);
+
+// ---------------------------------------------------------------- block-scaled values
+// mx.h gives the layout.  x / out: rows of ld elements, bf16 or fp32.
+void mx_quantize(hipStream_t st, const void* x, bool bf16, size_t ldx, int rows, int cols, int fmt, MxView q);
+void mx_dequantize(hipStream_t st, MxView q, int fmt, int rows, int cols, void* out, bool bf16, size_t ldo);
+// r = x + delta (delta NULL: x), stored in sum unless NULL (may be x); y = norm(r)
+// times gain[cols] unless NULL, written to q.  gather / n_dev as for norm_rows
+// (then without delta and sum); slots: the scale rows of q's groups.
+constexpr int ADD_NORM_MAX_COLS = 8192;
+struct AddNormMx {
+  const void* x = nullptr;
+  const void* delta = nullptr;
+  void* sum = nullptr;
+  const float* gain = nullptr;
+  const int32_t *gather = nullptr, *n_dev = nullptr;
+  size_t ldx = 0, ldd = 0, lds = 0, slots = 0, pitch = 0;
+  MxView q;
+  bool x_bf16 = false, delta_bf16 = false;
+  int rows = 0, cols = 0, pitch_cols = 0, norm_kind = 0, fmt = 0;
+  float eps = 0.0f;
+};
+void add_norm_mx(hipStream_t st, AddNormMx a);
+// C = A B^T of block-scaled A [M, K] (fmt_a) and B [N, K] (E2M1), fp32 accumulation,
+// to rows of ldo fp32 or bf16.  M_dev and rows_hint as for gemm_bf16; a row's
+// result does not depend on the launch's other rows.
+void mx_matmul(hipStream_t st, MxView A, int fmt_a, size_t a_slots, MxView B, int M, int N, int K,
+               const int* M_dev, void* out, bool out_bf16, size_t ldo, int rows_hint = -1);
+
+// ---------------------------------------------------------------- token scores
+// Of rows of V logits (fp32 or bf16, ld apart): log2 of the probability of
+// tokens[row] (tokens NULL: none), the entropy in bits, and the n_top largest
+// logits (equal ones by id) with the log2 of their probabilities.  ws: token_scores_ws
+// bytes, needed if that is not 0.
+size_t token_scores_ws(int n_rows, int V, int n_top);
+void token_scores(hipStream_t st, const void* logits, bool bf16, size_t ld, int n_rows, int V,
+                  const int32_t* tokens, int n_top, float* logp, float* entropy, int32_t* top_ids,
+                  float* top_logp, void* ws);
 
 }  // namespace dlmc

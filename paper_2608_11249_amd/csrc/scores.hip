@@ -1,0 +1,414 @@
+// Scores of logit rows: log2 probabilities of given tokens (their code lengths in
+// bits, negated), entropies, and the most probable alternatives, in one pass over
+// the logits.
+//
+// With t_i = (l_i - M) log2 e, M the row's largest logit: Z = sum 2^t_i, A = sum 2^t_i
+// t_i, log2 p_i = t_i - log2 Z, H = log2 Z - A / Z.  Every lane keeps its own running
+// M, Z, A and rescales them when its M rises.  (The difference comes first: l_i
+// log2 e would overflow in a row masked with the type's lowest value throughout.)
+//
+// Alternatives: each wave keeps a threshold that its k-th best so far reaches, and
+// collects the logits above it in LDS; a full list is cut to its k best, which
+// raises the threshold.  The first threshold is the k-th largest of the 64 lanes'
+// maxima of the wave's first tile.  A wave's tiles come in the order of their
+// columns, so among equal logits the ones collected first have the lowest ids, and
+// later ones equal to the threshold need not be looked at.
+#include "kernels.h"
+
+namespace dlmc {
+namespace {
+
+constexpr int TILE = 512;            // columns a wave takes at a time, eight a lane
+constexpr int LIST = 128 + TILE;     // a wave's list: cut above 128, then a whole tile fits
+constexpr int MAX_SPLIT = 32, MAX_TOP = 64;
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float NEG_INF = -__builtin_inff();
+
+struct Stat {
+  float M, Z, A;  // M = -inf: nothing above -inf (Z then 0, or NaN where a logit is NaN)
+};
+
+__device__ __forceinline__ Stat merge(Stat x, Stat y) {
+  if (y.M == NEG_INF) {
+    if (y.Z != y.Z) x.Z = x.A = y.Z;
+    return x;
+  }
+  if (x.M == NEG_INF) {
+    if (x.Z != x.Z) y.Z = y.A = x.Z;
+    return y;
+  }
+  // bounded, so that a sum scaled to nothing stays zero where the difference overflows
+  const float M = fmaxf(x.M, y.M);
+  const float dx = fmaxf((x.M - M) * LOG2E, -1.0e30f), dy = fmaxf((y.M - M) * LOG2E, -1.0e30f);
+  const float cx = __builtin_amdgcn_exp2f(dx), cy = __builtin_amdgcn_exp2f(dy);
+  return {M, fmaf(cx, x.Z, cy * y.Z), fmaf(cx, fmaf(dx, x.Z, x.A), cy * fmaf(dy, y.Z, y.A))};
+}
+
+// Order of logits as unsigned numbers, -0 as +0; and back.
+__device__ __forceinline__ uint32_t order_of(float v) {
+  const uint32_t u = __float_as_uint(v + 0.0f);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t k) {
+  return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
+}
+
+__device__ __forceinline__ int count(bool p) { return __popcll(__ballot(p)); }
+__device__ __forceinline__ int rank_in(uint64_t mask) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+
+// Keeps the k best of the entries key[e], id[e] (key 0: none) of a wave: sets keep[e]
+// and returns the k-th best's key, or 0 where there are no more than k.  Equal
+// keys: the lowest ids.
+template <int E>
+__device__ __forceinline__ uint32_t cut(const uint32_t (&key)[E], const uint32_t (&id)[E], int k, bool (&keep)[E]) {
+  uint32_t T = 0;
+  for (int bit = 31; bit >= 0; --bit) {  // the largest T that k keys reach
+    const uint32_t c = T | 1u << bit;
+    int n = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) n += count(key[e] >= c);
+    if (n >= k) T = c;
+  }
+  if (T == 0) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) keep[e] = key[e] != 0;
+    return 0;
+  }
+  int above = 0, ties = 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    above += count(key[e] > T);
+    ties += count(key[e] == T);
+  }
+  const int need = k - above;  // of the ties
+  uint32_t last = 0xFFFFFFFFu;
+  if (ties > need) {  // the largest id that fewer than `need` ties lie below
+    last = 0;
+    for (int bit = 30; bit >= 0; --bit) {
+      const uint32_t c = last | 1u << bit;
+      int n = 0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) n += count(key[e] == T && id[e] < c);
+      if (n < need) last = c;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) keep[e] = key[e] > T || (key[e] == T && id[e] <= last);
+  return T;
+}
+
+// The kept entries side by side in keys / ids; returns their number.
+template <int E>
+__device__ __forceinline__ int pack(const uint32_t (&key)[E], const uint32_t (&id)[E], const bool (&keep)[E],
+                                    uint32_t* keys, uint32_t* ids) {
+  int n = 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const uint64_t mask = __ballot(keep[e]);
+    if (keep[e]) {
+      const int at = n + rank_in(mask);
+      keys[at] = key[e];
+      ids[at] = id[e];
+    }
+    n += __popcll(mask);
+  }
+  return n;
+}
+
+// Descending order of (key, ~id) over the lanes of a wave.
+__device__ __forceinline__ void sort_lanes(uint32_t& key, uint32_t& id, int lane) {
+  for (int size = 2; size <= 64; size <<= 1)
+    for (int d = size >> 1; d > 0; d >>= 1) {
+      const uint32_t ok = __shfl_xor(key, d), oi = __shfl_xor(id, d);
+      const bool lower = (lane & d) == 0, down = (lane & size) == 0;
+      const bool mine_first = key > ok || (key == ok && id < oi);
+      if (mine_first != (lower == down)) {
+        key = ok;
+        id = oi;
+      }
+    }
+}
+
+struct ScoreArgs {
+  const void* logits;
+  size_t ld;
+  int n_rows, V, splits, k;
+  const int32_t* tokens;
+  float *logp, *entropy;
+  int32_t* top_ids;
+  float* top_logp;
+  // per (row, split), record_bytes(k) apart: (M, Z, A, 0), then k (key, id) pairs
+  uint8_t* ws;
+};
+
+__host__ __device__ inline size_t record_bytes(int k) { return 16 + 16 * (size_t)((k + 1) / 2); }
+
+// A row's results by one wave: its statistics and its k best, sorted over the lanes
+// (n of them; n = k where the row has a distribution).
+template <bool BF16>
+__device__ __forceinline__ void write_row(const ScoreArgs& p, int row, Stat s, uint32_t key, uint32_t id, int lane) {
+  // no distribution: nothing above -inf, a NaN, or an infinity
+  const bool ok = s.M > NEG_INF && s.M < -NEG_INF && s.Z == s.Z;
+  const float nan = __builtin_nanf(""), lz = ok ? log2f(s.Z) : nan;
+  if (lane < p.k) {
+    const size_t o = (size_t)row * p.k + lane;
+    p.top_ids[o] = ok ? (int32_t)id : -1;
+    p.top_logp[o] = ok ? (value_of(key) - s.M) * LOG2E - lz : nan;
+  }
+  if (lane != 0) return;
+  // a sum of nonnegative terms, up to rounding
+  const float h = lz - s.A / s.Z;
+  p.entropy[row] = ok ? (h < 0.0f ? 0.0f : h) : nan;
+  if (p.tokens) {
+    const int t = p.tokens[row];
+    float r = t == -1 ? 0.0f : nan;
+    if (ok && t >= 0 && t < p.V) {
+      const size_t at = (size_t)row * p.ld + t;
+      const float l = BF16 ? bf16_to_f32(((const bf16_t*)p.logits)[at]) : ((const float*)p.logits)[at];
+      r = (l - s.M) * LOG2E - lz;
+    }
+    p.logp[row] = r;
+  }
+}
+
+__device__ __forceinline__ Stat merge_lanes(Stat s) {
+  for (int o = 1; o < 64; o <<= 1) s = merge(s, Stat{__shfl_xor(s.M, o), __shfl_xor(s.Z, o), __shfl_xor(s.A, o)});
+  return s;
+}
+
+template <bool BF16, bool TOP>
+__global__ void __launch_bounds__(256)
+scores_kernel(ScoreArgs p) {
+  __shared__ uint32_t keys[TOP ? 4 : 1][TOP ? LIST : 1], ids[TOP ? 4 : 1][TOP ? LIST : 1];
+  __shared__ Stat stats[4];
+  __shared__ int counts[4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = blockIdx.x / p.splits, split = blockIdx.x % p.splits;
+  constexpr int CH = BF16 ? 8 : 4;  // columns of a 16-byte load
+  const uint8_t* base = (const uint8_t*)p.logits + (size_t)row * p.ld * (BF16 ? 2 : 4);
+  // columns are counted from the 16-byte border at or below the row's start
+  const int shift = (int)((uintptr_t)base / (BF16 ? 2 : 4) % CH);
+  const int nt = (p.V + shift + TILE - 1) / TILE;
+  const int per = (nt + 4 * p.splits - 1) / (4 * p.splits);
+  const int t0 = (split * 4 + wave) * per, t1 = min(t0 + per, nt);
+
+  auto column = [&](int t, int q) {  // first column of the lane's chunk q of tile t
+    return t * TILE - shift + (BF16 ? lane * 8 : q * 256 + lane * 4);
+  };
+  auto load = [&](int t, float (&v)[8]) {
+#pragma unroll
+    for (int q = 0; q < 8 / CH; ++q) {
+      const int c = column(t, q);
+      if (c >= 0 && c + CH <= p.V) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(base + (size_t)c * (BF16 ? 2 : 4));
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+          v[q * CH + i] = BF16 ? __uint_as_float(i % 2 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16) : __uint_as_float(w[i % 4]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+          v[q * CH + i] = NEG_INF;
+          if (c + i >= 0 && c + i < p.V)
+            v[q * CH + i] = BF16 ? bf16_to_f32(((const bf16_t*)base)[c + i]) : ((const float*)base)[c + i];
+        }
+      }
+    }
+  };
+
+  Stat s{NEG_INF, 0.0f, 0.0f};
+  float thr = NEG_INF;
+  int n = 0;
+  uint32_t* wk = keys[TOP ? wave : 0];
+  uint32_t* wi = ids[TOP ? wave : 0];
+  auto shrink = [&] {
+    constexpr int E = LIST / 64;
+    uint32_t key[E], id[E];
+    bool keep[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int at = e * 64 + lane;
+      key[e] = at < n ? wk[at] : 0u;
+      id[e] = at < n ? wi[at] : 0xFFFFFFFFu;
+    }
+    const uint32_t T = cut<E>(key, id, p.k, keep);
+    if (T == 0) return;
+    n = pack<E>(key, id, keep, wk, wi);
+    thr = value_of(T);
+  };
+
+  auto take = [&](int t, const float (&v)[8]) {
+    float top = v[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) top = fmaxf(top, v[i]);
+    if (top > s.M) {
+      if (s.M > NEG_INF) {
+        const float d = fmaxf((s.M - top) * LOG2E, -1.0e30f), c = __builtin_amdgcn_exp2f(d);
+        s.A = c * fmaf(d, s.Z, s.A);
+        s.Z *= c;
+      }
+      s.M = top;
+    }
+    if (s.M > NEG_INF) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = (v[i] - s.M) * LOG2E, e = __builtin_amdgcn_exp2f(x);
+        s.Z += e;
+        s.A = fmaf(e, fmaxf(x, -1.0e30f), s.A);  // -inf: adds 0
+      }
+    } else {  // the max passes over NaN
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (v[i] != v[i]) s.Z = s.A = v[i];
+    }
+    if constexpr (TOP) {
+      if (t == t0) {  // the k-th largest lane maximum: k values reach it
+        uint32_t key = order_of(top == top ? top : NEG_INF), id = 0;
+        sort_lanes(key, id, lane);
+        thr = value_of(__shfl(key, p.k - 1));
+      }
+      const bool fill = n < p.k;  // ties with the threshold count
+      if (__any(fill ? top >= thr : top > thr)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int c = column(t, i / CH) + i % CH;
+          const bool in = (fill ? v[i] >= thr : v[i] > thr) && c >= 0 && c < p.V;
+          const uint64_t mask = __ballot(in);
+          if (in) {
+            const int at = n + rank_in(mask);
+            wk[at] = order_of(v[i]);
+            wi[at] = (uint32_t)c;
+          }
+          n += __popcll(mask);
+        }
+        if (n > LIST - TILE) shrink();
+      }
+    }
+  };
+
+  int t = t0;
+  for (; t + 1 < t1; t += 2) {
+    float a[8], b[8];
+    load(t, a);
+    load(t + 1, b);
+    take(t, a);
+    take(t + 1, b);
+  }
+  if (t < t1) {
+    float a[8];
+    load(t, a);
+    take(t, a);
+  }
+
+  if constexpr (TOP) {
+    shrink();
+    if (lane == 0) counts[wave] = n;
+  }
+  s = merge_lanes(s);
+  if (lane == 0) stats[wave] = s;
+  __syncthreads();
+  if (wave != 0) return;
+  s = merge(merge(stats[0], stats[1]), merge(stats[2], stats[3]));
+  uint32_t key = 0, id = 0xFFFFFFFFu;
+  if constexpr (TOP) {
+    uint32_t k4[4], i4[4];
+    bool keep[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool in = lane < counts[e];
+      k4[e] = in ? keys[e][lane] : 0u;
+      i4[e] = in ? ids[e][lane] : 0xFFFFFFFFu;
+    }
+    cut<4>(k4, i4, p.k, keep);
+    n = pack<4>(k4, i4, keep, wk, wi);
+    if (lane < n) {
+      key = wk[lane];
+      id = wi[lane];
+    }
+  }
+  if (p.splits == 1) {
+    if constexpr (TOP) sort_lanes(key, id, lane);
+    write_row<BF16>(p, row, s, key, id, lane);
+    return;
+  }
+  uint8_t* w = p.ws + (size_t)blockIdx.x * record_bytes(p.k);
+  if (lane == 0) *reinterpret_cast<f32x4*>(w) = f32x4{s.M, s.Z, s.A, 0.0f};
+  if (lane < p.k) *reinterpret_cast<u32x2*>(w + 16 + 8 * lane) = u32x2{key, id};
+}
+
+// The splits of a row joined, by one wave a row.
+template <bool BF16>
+__global__ void __launch_bounds__(64)
+scores_join_kernel(ScoreArgs p) {
+  __shared__ uint32_t keys[MAX_TOP], ids[MAX_TOP];
+  const int row = blockIdx.x, lane = threadIdx.x;
+  const size_t rec = record_bytes(p.k);
+  const uint8_t* w = p.ws + (size_t)row * p.splits * rec;
+  Stat s{NEG_INF, 0.0f, 0.0f};
+  if (lane < p.splits) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(w + lane * rec);
+    s = Stat{v[0], v[1], v[2]};
+  }
+  s = merge_lanes(s);
+  uint32_t key = 0, id = 0xFFFFFFFFu;
+  if (p.k) {
+    // split e's entries by the lanes, all k of them valid where it has that many
+    constexpr int E = MAX_SPLIT;
+    uint32_t ke[E], ie[E];
+    bool keep[E];
+    const bool in = lane < p.k;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      u32x2 x{0u, 0xFFFFFFFFu};
+      if (in && e < p.splits) x = *reinterpret_cast<const u32x2*>(w + e * rec + 16 + 8 * lane);
+      ke[e] = x[0];
+      ie[e] = x[1];
+    }
+    cut<E>(ke, ie, p.k, keep);
+    const int n = pack<E>(ke, ie, keep, keys, ids);
+    if (lane < n) {
+      key = keys[lane];
+      id = ids[lane];
+    }
+    sort_lanes(key, id, lane);
+  }
+  write_row<BF16>(p, row, s, key, id, lane);
+}
+
+// Blocks a row's columns are split over: enough blocks for the chip's 256 CUs eight
+// times over, but at least two tiles to a wave.
+int splits_of(int n_rows, int V) {
+  const int most = std::max(1, std::min(MAX_SPLIT, V / (8 * TILE)));
+  return std::max(1, std::min(most, 2048 / std::max(n_rows, 1)));
+}
+
+}  // namespace
+
+size_t token_scores_ws(int n_rows, int V, int n_top) {
+  const int s = splits_of(n_rows, V);
+  return s == 1 ? 0 : (size_t)n_rows * s * record_bytes(n_top);
+}
+
+void token_scores(hipStream_t st, const void* logits, bool bf16, size_t ld, int n_rows, int V, const int32_t* tokens,
+                  int n_top, float* logp, float* entropy, int32_t* top_ids, float* top_logp, void* ws) {
+  if (n_rows <= 0) return;
+  DLMC_CHECK(n_top >= 0 && n_top <= MAX_TOP && n_top <= V, DLMC_E_INVAL, "alternatives a row");
+  ScoreArgs p{logits, ld, n_rows, V, splits_of(n_rows, V), n_top, tokens, logp, entropy, top_ids, top_logp, (uint8_t*)ws};
+  const unsigned grid = (unsigned)n_rows * p.splits;
+  if (bf16) {
+    if (n_top) scores_kernel<true, true><<<grid, 256, 0, st>>>(p);
+    else scores_kernel<true, false><<<grid, 256, 0, st>>>(p);
+  } else {
+    if (n_top) scores_kernel<false, true><<<grid, 256, 0, st>>>(p);
+    else scores_kernel<false, false><<<grid, 256, 0, st>>>(p);
+  }
+  DLMC_HIP(hipGetLastError());
+  if (p.splits > 1) {
+    if (bf16) scores_join_kernel<true><<<n_rows, 64, 0, st>>>(p);
+    else scores_join_kernel<false><<<n_rows, 64, 0, st>>>(p);
+    DLMC_HIP(hipGetLastError());
+  }
+}
+
+}  // namespace dlmc
