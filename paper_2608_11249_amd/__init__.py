@@ -181,13 +181,54 @@ class MXMatrix:
     rows: int
     cols: int
 
+    def shapes(self):
+        """The shapes of codes and scales."""
+        groups = -(-self.cols // 256)
+        return ((self.rows, groups * (128 if self.fmt == "fp4" else 256)), (groups, -(-self.rows // 32) * 32, 8))
+
+    @staticmethod
+    def like(t, fmt: str, rows: int, cols: int) -> "MXMatrix":
+        """One to be filled, on the device of tensor t."""
+        q = MXMatrix(None, None, fmt, rows, cols)
+        codes, scales = q.shapes()
+        u8 = _torch().uint8
+        q.codes, q.scales = t.new_empty(codes, dtype=u8), t.new_empty(scales, dtype=u8)
+        return q
+
     @staticmethod
     def empty(fmt: str, rows: int, cols: int, device) -> "MXMatrix":
+        """One to be filled, on `device`."""
+        return MXMatrix.like(_torch().empty(0, device=device), fmt, rows, cols)
+
+
+_torch_module = _types = _raw = None
+
+
+def _torch():
+    global _torch_module
+    if _torch_module is None:
         import torch
-        groups = -(-cols // 256)
-        codes = torch.empty((rows, groups * (128 if fmt == "fp4" else 256)), dtype=torch.uint8, device=device)
-        scales = torch.empty((groups, -(-rows // 32) * 32, 8), dtype=torch.uint8, device=device)
-        return MXMatrix(codes, scales, fmt, rows, cols)
+        _torch_module = torch
+    return _torch_module
+
+
+def _type_codes():
+    """Element types of the calls on block-scaled values and scores."""
+    global _types
+    if _types is None:
+        _types = {_torch().float32: DTYPE["f32"], _torch().bfloat16: DTYPE["bf16"]}
+    return _types
+
+
+def _raw_stream(device: int) -> int:
+    """The handle of torch's current stream on GPU `device` (0: the default one)."""
+    global _raw
+    if _raw is None:
+        torch = _torch()
+        # without the Stream object, where torch offers that: 2 us a call
+        _raw = getattr(torch._C, "_cuda_getCurrentRawStream",
+                       lambda d: torch.cuda.current_stream(d).cuda_stream)
+    return _raw(device)
 
 
 def model_config(shape, max_chunk: int, max_batch: int) -> ModelConfig:
@@ -400,11 +441,14 @@ class Model:
         fills its tensors (which live until it returns).  The default stream's
         handle is 0, for which the library would take its own stream."""
         import torch
-        stream = torch.cuda.current_stream(device).cuda_stream or DEFAULT_STREAM
+        self._follow(torch.cuda.current_stream(device).cuda_stream)
+        _check(fn(self.handle, *(_ptr(a) if torch.is_tensor(a) else a for a in args)))
+
+    def _follow(self, handle: int):
+        stream = handle or DEFAULT_STREAM
         if stream != self._stream:
             self.set_stream(stream)
             self._hook_stream = stream == DEFAULT_STREAM
-        _check(fn(self.handle, *(_ptr(a) if torch.is_tensor(a) else a for a in args)))
 
     def forward_logits(self, state):
         """state: int32 cuda tensor [B, T].  Returns (logits [n, V], rows [n])."""
@@ -494,46 +538,59 @@ class Model:
         return sel_pos, sel_row, n_sel
 
     # ---- block-scaled values and token scores (torch device tensors; the calls
-    # return without waiting for the GPU)
-    def _rows(self, t, what: str, cols: Optional[int] = None):
-        """(DTYPE code, row distance) of a 2-d fp32 or bf16 tensor on this GPU whose
-        rows are contiguous; `cols` if it has to have that many columns."""
-        import torch
-        if not torch.is_tensor(t) or t.dim() != 2:
-            _refuse(f"{what} must be a 2-d tensor")
-        code = 0 if t.dtype == torch.float32 else 1 if t.dtype == torch.bfloat16 else _refuse(
-            f"{what} must be float32 or bfloat16, not {t.dtype}")
-        self._here(t, what)
-        if cols is not None and t.shape[1] != cols:
-            _refuse(f"{what} must have {cols} columns, not {t.shape[1]}")
-        if t.shape[1] > 1 and t.stride(1) != 1:
-            _refuse(f"{what} must have contiguous rows")
-        if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
-            _refuse(f"{what}: rows overlap")
-        return code, t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    # return without waiting for the GPU, so what they cost a short launch is the
+    # host's time: one pass of checks, no copies, raw pointers)
+    def _call(self, fn, *args):
+        self._follow(_raw_stream(self.device))
+        st = fn(self.handle, *args)
+        if st:
+            _check(st)
 
     def _here(self, t, what: str):
-        if t.device.type != "cuda" or t.device.index != self.device:
+        if t.get_device() != self.device:
             _refuse(f"{what} must be on the model's GPU (cuda:{self.device}), not on {t.device}")
 
+    def _rows(self, t, what: str, cols: Optional[int] = None):
+        """(type code, row distance, pointer) of a 2-d fp32 or bf16 tensor on this
+        GPU whose rows are contiguous; `cols` if it has to have that many columns."""
+        code = _type_codes().get(getattr(t, "dtype", None))
+        if code is None:
+            _refuse(f"{what} must be a float32 or bfloat16 tensor")
+        if t.dim() != 2:
+            _refuse(f"{what} must be 2-d")
+        if t.get_device() != self.device:
+            self._here(t, what)
+        n, c = t.shape
+        if cols is not None and c != cols:
+            _refuse(f"{what} must have {cols} columns, not {c}")
+        ld, step = t.stride()
+        if c > 1 and step != 1:
+            _refuse(f"{what} must have contiguous rows")
+        if n <= 1:
+            ld = c
+        elif ld < c:
+            _refuse(f"{what}: rows overlap")
+        return code, ld, t.data_ptr()
+
     def _vector(self, t, what: str, n: int, dtype):
-        import torch
-        if not torch.is_tensor(t) or t.dtype != dtype or t.dim() != 1 or t.shape[0] != n:
+        if getattr(t, "dtype", None) != dtype or t.dim() != 1 or t.shape[0] != n:
             _refuse(f"{what} must be a tensor of {n} {dtype} values")
         self._here(t, what)
         return t.contiguous()
 
     def _held(self, q, what: str, fmt: Optional[str] = None):
+        """(codes, scales) pointers of an MXMatrix on this GPU whose arrays fit it."""
         if not isinstance(q, MXMatrix) or q.fmt not in MX_FORMAT or q.rows < 0 or not 1 <= q.cols <= 1 << 24:
             _refuse(f"{what} must be an MXMatrix")
         if fmt is not None and q.fmt != fmt:
             _refuse(f"{what} must be held in {fmt}, not in {q.fmt}")
-        groups = -(-q.cols // 256)
-        for t, shape in ((q.codes, (q.rows, groups * (128 if q.fmt == "fp4" else 256))),
-                         (q.scales, (groups, -(-q.rows // 32) * 32, 8))):
-            if tuple(t.shape) != shape or not t.is_contiguous() or t.element_size() != 1:
-                _refuse(f"{what}: codes or scales do not fit {q.rows} x {q.cols} in {q.fmt}")
-            self._here(t, what)
+        c, s = q.codes, q.scales
+        if ((c.shape, s.shape) != q.shapes() or c.element_size() != 1 or s.element_size() != 1
+                or not (c.is_contiguous() and s.is_contiguous())):
+            _refuse(f"{what}: codes or scales do not fit {q.rows} x {q.cols} in {q.fmt}")
+        self._here(c, what)
+        self._here(s, what)
+        return c.data_ptr(), s.data_ptr()
 
     @staticmethod
     def _format(fmt: str) -> int:
@@ -541,28 +598,30 @@ class Model:
 
     @staticmethod
     def _out_type(dtype) -> int:
-        import torch
-        return 0 if dtype == torch.float32 else 1 if dtype == torch.bfloat16 else _refuse(
-            f"output type must be float32 or bfloat16, not {dtype}")
+        code = _type_codes().get(dtype)
+        return _refuse(f"output type must be float32 or bfloat16, not {dtype}") if code is None else code
 
     def mx_quantize(self, x, fmt: str = "fp4") -> MXMatrix:
         """x [rows, cols] (fp32 or bf16) in E2M1 ("fp4") or E4M3 ("fp8") with a
         power-of-two scale for each 32 columns; nothing saturates."""
-        code, ld = self._rows(x, "x")
+        code, ld, ptr = self._rows(x, "x")
         f = self._format(fmt)
-        q = MXMatrix.empty(fmt, x.shape[0], x.shape[1], x.device)
-        self._on_current_stream(x.device, lib().dlmc_mx_quantize, x, code, ld, q.rows, q.cols, f, q.codes, q.scales)
+        rows, cols = x.shape
+        if not 1 <= cols <= 1 << 24:
+            _refuse("x must have 1 to 2^24 columns")
+        q = MXMatrix.like(x, fmt, rows, cols)
+        self._call(lib().dlmc_mx_quantize, ptr, code, ld, rows, cols, f, q.codes.data_ptr(), q.scales.data_ptr())
         return q
 
     def mx_dequantize(self, q: MXMatrix, dtype=None):
         """The values that q holds, bf16 (the default: exact) or fp32 [rows, cols]."""
-        import torch
+        torch = _torch()
         dtype = torch.bfloat16 if dtype is None else dtype
         code = self._out_type(dtype)
-        self._held(q, "q")
-        out = torch.empty((q.rows, q.cols), dtype=dtype, device=q.codes.device)
-        self._on_current_stream(out.device, lib().dlmc_mx_dequantize, q.codes, q.scales, MX_FORMAT[q.fmt], q.rows,
-                                q.cols, out, code, q.cols)
+        codes, scales = self._held(q, "q")
+        out = q.codes.new_empty((q.rows, q.cols), dtype=dtype)
+        self._call(lib().dlmc_mx_dequantize, codes, scales, MX_FORMAT[q.fmt], q.rows, q.cols, out.data_ptr(), code,
+                   q.cols)
         return out
 
     def add_norm_mx(self, x, delta=None, gain=None, fmt: str = "fp8", norm: Optional[str] = None,
@@ -570,76 +629,85 @@ class Model:
         """(r, q): r = x + delta [rows, cols] in x's type (x itself without a delta;
         written to `out`, which may be x, if given) and its norm times gain (fp32)
         as an MXMatrix.  norm ("rmsnorm" or "layernorm") and eps: the model's."""
-        import torch
-        code, ld = self._rows(x, "x")
+        code, ld, ptr = self._rows(x, "x")
         rows, cols = x.shape
-        kind = self.shape.norm if norm is None else norm
-        if kind not in NORM:
-            _refuse(f"norm must be rmsnorm or layernorm, not {kind!r}")
-        dcode, ldd = self._rows(delta, "delta", cols) if delta is not None else (0, 0)
-        if delta is not None and delta.shape[0] != rows:
-            _refuse(f"delta must have {rows} rows, not {delta.shape[0]}")
+        kind = NORM.get(self.shape.norm if norm is None else norm)
+        if kind is None:
+            _refuse(f"norm must be rmsnorm or layernorm, not {norm!r}")
+        if not 1 <= cols <= 8192:
+            _refuse("a norm takes 1 to 8192 columns")
+        dcode = ldd = lds = 0
+        dptr = gptr = sptr = None
+        if delta is not None:
+            dcode, ldd, dptr = self._rows(delta, "delta", cols)
+            if delta.shape[0] != rows:
+                _refuse(f"delta must have {rows} rows, not {delta.shape[0]}")
         f = self._format(fmt)
         if gain is not None:
-            gain = self._vector(gain, "gain", cols, torch.float32)
-        if out is None:
-            r = x if delta is None else torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-            total = None if delta is None else r
-        else:
-            r = total = out
-        lds = 0
-        if total is not None:
-            ocode, lds = self._rows(total, "out", cols)
-            if ocode != code or total.shape[0] != rows:
+            gain = self._vector(gain, "gain", cols, _torch().float32)
+            gptr = gain.data_ptr()
+        if out is not None:
+            r = out
+            ocode, lds, sptr = self._rows(out, "out", cols)
+            if ocode != code or out.shape[0] != rows:
                 _refuse("out must have x's shape and type")
-        q = MXMatrix.empty(fmt, rows, cols, x.device)
-        self._on_current_stream(x.device, lib().dlmc_add_norm_mx, x, code, ld, delta, dcode, ldd, total, lds, gain,
-                                NORM[kind], self.shape.norm_eps if eps is None else eps, rows, cols, f, q.codes,
-                                q.scales)
+        elif delta is None:
+            r = x
+        else:
+            r = x.new_empty((rows, cols))
+            lds, sptr = cols, r.data_ptr()
+        q = MXMatrix.like(x, fmt, rows, cols)
+        self._call(lib().dlmc_add_norm_mx, ptr, code, ld, dptr, dcode, ldd, sptr, lds, gptr, kind,
+                   self.shape.norm_eps if eps is None else eps, rows, cols, f, q.codes.data_ptr(),
+                   q.scales.data_ptr())
         return r, q
 
     def mx_matmul(self, a: MXMatrix, b: MXMatrix, out_dtype=None, out=None):
         """a b^T [a.rows, b.rows] of a in either format and b in E2M1, accumulated in
         fp32, as fp32 (the default) or bf16, into `out` if given."""
-        import torch
-        self._held(a, "a")
-        self._held(b, "b", "fp4")
-        if a.cols != b.cols:
-            _refuse(f"a has {a.cols} columns, b {b.cols}")
+        ac, asc = self._held(a, "a")
+        bc, bsc = self._held(b, "b", "fp4")
+        M, N, K = a.rows, b.rows, a.cols
+        if K != b.cols:
+            _refuse(f"a has {K} columns, b {b.cols}")
         if out is None:
-            dtype = torch.float32 if out_dtype is None else out_dtype
-            code, ldo = self._out_type(dtype), b.rows
-            out = torch.empty((a.rows, b.rows), dtype=dtype, device=a.codes.device)
+            dtype = _torch().float32 if out_dtype is None else out_dtype
+            code, ldo = self._out_type(dtype), N
+            out = a.codes.new_empty((M, N), dtype=dtype)
+            optr = out.data_ptr()
         else:
-            code, ldo = self._rows(out, "out", b.rows)
-            if out.shape[0] != a.rows or (out_dtype is not None and out.dtype != out_dtype):
+            code, ldo, optr = self._rows(out, "out", N)
+            if out.shape[0] != M or (out_dtype is not None and out.dtype != out_dtype):
                 _refuse("out does not have the product's shape and type")
-        self._on_current_stream(out.device, lib().dlmc_mx_matmul, a.codes, a.scales, MX_FORMAT[a.fmt], b.codes,
-                                b.scales, a.rows, b.rows, a.cols, out, code, ldo)
+        self._call(lib().dlmc_mx_matmul, ac, asc, MX_FORMAT[a.fmt], bc, bsc, M, N, K, optr, code, ldo)
         return out
 
     def token_scores(self, logits, tokens=None, top: int = 0):
         """Of logits [n, vocab] (fp32 or bf16): (log2 probability of tokens[i] in row
         i (None without tokens), entropy in bits, ids [n, top] of the most probable
         symbols, their log2 probabilities)."""
-        import torch
+        torch = _torch()
         V = self.shape.vocab
-        code, ld = self._rows(logits, "logits", V)
-        n, dev = logits.shape[0], logits.device
+        code, ld, ptr = self._rows(logits, "logits", V)
+        n = logits.shape[0]
         if not 0 <= top <= min(64, V):
             _refuse("top must be in 0..64, at most the vocabulary")
-        logp = None
+        logp = tptr = lptr = None
+        f32t, i32t = torch.float32, torch.int32
         if tokens is not None:
-            tokens = self._vector(tokens, "tokens", n, torch.int32)
-            logp = torch.empty(n, dtype=torch.float32, device=dev)
-        H = torch.empty(n, dtype=torch.float32, device=dev)
-        ids = torch.empty((n, top), dtype=torch.int32, device=dev)
-        tlp = torch.empty((n, top), dtype=torch.float32, device=dev)
+            tokens = self._vector(tokens, "tokens", n, i32t)
+            logp = logits.new_empty(n, dtype=f32t)
+            tptr, lptr = tokens.data_ptr(), logp.data_ptr()
+        H = logits.new_empty(n, dtype=f32t)
+        ids = logits.new_empty((n, top), dtype=i32t)
+        tlp = logits.new_empty((n, top), dtype=f32t)
         need = u64(0)
-        _check(lib().dlmc_token_scores_ws(self.handle, n, top, ctypes.byref(need)))
-        ws = torch.empty(need.value, dtype=torch.uint8, device=dev) if need.value else None
-        self._on_current_stream(dev, lib().dlmc_token_scores, logits, code, ld, n, tokens, top, logp, H, ids, tlp,
-                                ws, need.value)
+        L = lib()
+        _check(L.dlmc_token_scores_ws(self.handle, n, top, ctypes.byref(need)))
+        need = need.value
+        ws = logits.new_empty(need, dtype=torch.uint8) if need else None
+        self._call(L.dlmc_token_scores, ptr, code, ld, n, tptr, top, lptr, H.data_ptr(), ids.data_ptr(),
+                   tlp.data_ptr(), ws.data_ptr() if need else None, need)
         return logp, H, ids, tlp
 
     def weight(self, tensor_id: int, rows: int, cols: int) -> np.ndarray:

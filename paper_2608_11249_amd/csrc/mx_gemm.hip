@@ -21,6 +21,9 @@
 // the launch's other rows.
 #include "kernels.h"
 
+#include <type_traits>
+#include <utility>
+
 namespace dlmc {
 namespace {
 
@@ -40,15 +43,26 @@ __device__ __forceinline__ void bare_barrier() {
   asm volatile("" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
 }
-// s_waitcnt immediate: vmcnt(n) alone
+// s_waitcnt immediates: vmcnt(n) alone, and with lgkmcnt(0)
 constexpr int wait_vm(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }
+constexpr int wait_vm_lds(int n) { return 0x0070 | (n & 15) | ((n >> 4) << 14); }
+
+template <int B0, typename F, int... I>
+__device__ __forceinline__ void static_for_impl(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, B0 + I>{}), ...);
+}
+// f(integral_constant<B0>) ... f(integral_constant<B1 - 1>)
+template <int B0, int B1, typename F>
+__device__ __forceinline__ void static_for(F&& f) {
+  static_for_impl<B0>(f, std::make_integer_sequence<int, (B1 > B0 ? B1 - B0 : 0)>{});
+}
 
 // 16-byte chunks of a tile row are stored XOR-swizzled, so that the 16 rows that a
-// ds_read_b128 serves at a time fall on the 16 slots of the 64 banks: rows of 128
-// bytes by (row / 2) % 8, rows of 256 bytes by row % 16.
+// ds_read_b128 serves at a time fall on the 16 slots of the 64 banks: rows of 64
+// bytes by (row / 4) % 4, of 128 bytes by (row / 2) % 8, of 256 bytes by row % 16.
 template <int ROW>
 __device__ __forceinline__ int swizzle(int row) {
-  return ROW == 128 ? (row >> 1) & 7 : row & 15;
+  return ROW == 64 ? (row >> 2) & 3 : ROW == 128 ? (row >> 1) & 7 : row & 15;
 }
 
 // This block's tile among those with live rows; hardware block ids go round robin
@@ -73,6 +87,7 @@ struct MxArgs {
   void* out;
   size_t ldo;
   int n_tm, n_tn;
+  int past_caches;  // the output is larger than the caches keep
 };
 
 // BM x BN tiles by WR x WC waves, a ring of NS stages of one group (256 columns)
@@ -226,6 +241,281 @@ mx_ring_kernel(MxArgs p) {
     }
 }
 
+// ---------------------------------------------------------------------------
+// 256 x 256 tiles by four waves, one per SIMD, each on 128 x 128 (256 accumulator
+// registers).  A wave reads eight fragments for sixteen instructions, and a tile
+// fills LDS with 68 KB (E2M1) or 100 KB (E4M3) per 256 columns, half as much per
+// product as 128-wide tiles: filling and reading LDS is what bounds these kernels.
+//
+// LDS holds a ring of NS stages of 128 columns of both operands (half a group), and
+// two slots of a group's scales.  A stage is two steps of 64 columns; fragments are
+// read one step ahead.  Between a stage's steps each wave waits until its loads of
+// the next stage have landed and its fragment reads are done, then a barrier frees
+// the stage; the loads of the stage NS later go there, one at a time between the
+// instructions of the next two steps (issued together they would hold up the
+// instructions behind them).
+//
+// Loads of a stage are issued in two halves: the first after the barrier of stage
+// u - NS (with the group's scales if u is even), the second before that of stage
+// u - NS + 1.  The last two groups are peeled, so the main loop has no branches.
+//
+// Whether stage t + d exists in group R from the end (t = 2 ng - 4 + 2 R).
+constexpr bool wide_exists(int R, int d) { return R < 0 || 2 * R - 4 + d < 0; }
+// Loads issued after those of stage t + st + 1, when the barrier of stage t + st is
+// near: the whole stages up to t + st + NS - 1.
+constexpr int wide_younger(int NS, int NL, int R, int st) {
+  int n = 0;
+  for (int v = st + 2; v <= st + NS - 1; ++v)
+    if (wide_exists(R, v)) n += NL + (v % 2 == 0);
+  return n;
+}
+
+template <int FA, int TM, int NS, bool OUT_BF16>
+__global__ void __launch_bounds__(256, TM == 2 ? 2 : 1)
+mx_wide_kernel(MxArgs p) {
+  constexpr int WM = 32 * TM, BM = 2 * WM;
+  constexpr int AROW = FA == DLMC_MX_FP4 ? 64 : 128, BROW = 64;  // bytes of a row in a stage
+  constexpr int A_B = BM * AROW, B_B = 256 * BROW, STAGE = A_B + B_B, SC = 4096;
+  constexpr int A_IN = A_B / 4096, B_IN = B_B / 4096, NL = A_IN + B_IN, H1 = NS == 2 ? NL : NL / 2;
+  constexpr int PF = 256 + 8;  // pitch of the staged output, in its elements
+  constexpr int LDS = NS * STAGE + 2 * SC, OUT = OUT_BF16 ? BM * PF * 2 : 0;
+  static_assert(LDS <= (TM == 2 ? 80 : 160) * 1024 && OUT <= (TM == 2 ? 80 : 160) * 1024, "LDS");
+  __shared__ __attribute__((aligned(16))) uint8_t smem[LDS > OUT ? LDS : OUT];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave >> 1, wn = wave & 1, lr = lane & 31, lg = lane >> 5;
+  const int Mv = p.M_dev ? min(*p.M_dev, p.M) : p.M;
+  int tm, tn;
+  if (!tile_of(blockIdx.x, p.n_tm, p.n_tn, BM, Mv, tm, tn)) return;
+  const int m0 = tm * BM, n0 = tn * 256, ng = p.groups;
+
+  const uint32_t a_pitch = (uint32_t)ng * (2 * AROW), b_pitch = (uint32_t)ng * (2 * BROW);
+  const uint8_t* a_base = p.a + (size_t)m0 * a_pitch;
+  const uint8_t* b_base = p.b + (size_t)n0 * b_pitch;
+  uint32_t a_off[A_IN], b_off[B_IN];
+#pragma unroll
+  for (int j = 0; j < A_IN; ++j) {
+    const int slot = (wave * A_IN + j) * 64 + lane, row = slot / (AROW / 16), c = slot % (AROW / 16);
+    a_off[j] = (uint32_t)min(row, Mv - 1 - m0) * a_pitch + ((c ^ swizzle<AROW>(row)) << 4);
+  }
+#pragma unroll
+  for (int j = 0; j < B_IN; ++j) {
+    const int slot = (wave * B_IN + j) * 64 + lane, row = slot / (BROW / 16), c = slot % (BROW / 16);
+    b_off[j] = (uint32_t)min(row, p.N - 1 - n0) * b_pitch + ((c ^ swizzle<BROW>(row)) << 4);
+  }
+  // scales: the first BM / 128 waves load A's rows, the next two B's, two rows a
+  // lane (a fourth wave without any loads some again, into a place of its own)
+  const bool s_a = wave * 128 < BM;
+  const uint8_t* s_base = s_a ? p.as : p.bs;
+  const size_t s_slots = s_a ? p.a_slots : p.b_slots;
+  const size_t s_row = min((size_t)((s_a ? m0 + wave * 128 : n0 + wave * 128 - BM) + lane * 2), s_slots - 2);
+  const uint8_t* s_src = s_base + s_row * 8;
+
+  // load I of stage u
+  auto load = [&](int u, auto i_) {
+    constexpr int I = decltype(i_)::value;
+    uint8_t* st = smem + (u % NS) * STAGE;
+    if constexpr (I < A_IN)
+      dma16(a_base + (size_t)u * AROW + a_off[I], st + (wave * A_IN + I) * 1024);
+    else
+      dma16(b_base + (size_t)u * BROW + b_off[I - A_IN], st + A_B + (wave * B_IN + I - A_IN) * 1024);
+  };
+  auto load_scales = [&](int g) {
+    dma16(s_src + (size_t)g * s_slots * 8, smem + NS * STAGE + (g & 1) * SC + wave * 1024);
+  };
+  typedef i32x4 FragB;
+  struct FragA {
+    i32x4 q[FA == DLMC_MX_FP4 ? 1 : 2];
+  };
+  auto frag_a = [&](FragA& f, const uint8_t* st, int s, int i) {
+    const int row = wm * WM + i * 32 + lr, x = swizzle<AROW>(row);
+    if constexpr (FA == DLMC_MX_FP4) {
+      f.q[0] = *reinterpret_cast<const i32x4*>(st + row * AROW + (((2 * s + lg) ^ x) << 4));
+    } else {
+      f.q[0] = *reinterpret_cast<const i32x4*>(st + row * AROW + (((4 * s + lg) ^ x) << 4));
+      f.q[1] = *reinterpret_cast<const i32x4*>(st + row * AROW + (((4 * s + 2 + lg) ^ x) << 4));
+    }
+  };
+  auto frag_b = [&](FragB& f, const uint8_t* st, int s, int j) {
+    const int row = wn * 128 + j * 32 + lr;
+    f = *reinterpret_cast<const i32x4*>(st + A_B + row * BROW + (((2 * s + lg) ^ swizzle<BROW>(row)) << 4));
+  };
+  auto read_scales = [&](u32x2 (&sa)[TM], u32x2 (&sb)[4], int g) {
+    const uint8_t* sc = smem + NS * STAGE + (g & 1) * SC;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) sa[i] = *reinterpret_cast<const u32x2*>(sc + (wm * WM + i * 32 + lr) * 8);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sb[i] = *reinterpret_cast<const u32x2*>(sc + (BM + wn * 128 + i * 32 + lr) * 8);
+  };
+
+  f32x16 acc[TM][4];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+
+  // prologue: stages 0 .. NS - 2 and the first half of stage NS - 1
+  const int nst = 2 * ng;
+  static_for<0, NS>([&](auto u_) {
+    constexpr int U = decltype(u_)::value;
+    if (U < nst) {
+      if constexpr (U % 2 == 0) load_scales(U / 2);
+      static_for<0, U == NS - 1 ? H1 : NL>([&](auto i_) { load(U, i_); });
+    }
+  });
+  // younger than stage 0: stages 1 .. NS - 2, the half, and the scales of even ones
+  constexpr int AFTER0 = (NS - 2) * NL + H1 + (NS - 1) / 2;
+  if (nst >= NS)
+    __builtin_amdgcn_s_waitcnt(wait_vm(AFTER0));
+  else
+    __builtin_amdgcn_s_waitcnt(wait_vm(0));
+  bare_barrier();
+  FragA fa[2][TM];
+  FragB fb[2][4];
+  u32x2 sa[TM], sb[4], na[TM], nb[4];
+#pragma unroll
+  for (int i = 0; i < TM; ++i) frag_a(fa[0][i], smem, 0, i);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) frag_b(fb[0][i], smem, 0, i);
+  read_scales(na, nb, 0);
+
+  // One group.  R < 0: every load exists; R = 0, 1: the last but one and the last
+  // group, loads of stages past the end dropped.
+  auto trip = [&](int g, auto r_) {
+    constexpr int R = decltype(r_)::value;
+    const int t = 2 * g;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) sa[i] = u32x2{na[i][0] >> (8 * lg), na[i][1] >> (8 * lg)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sb[i] = u32x2{nb[i][0] >> (8 * lg), nb[i][1] >> (8 * lg)};
+    auto step = [&](auto x_) {
+      constexpr int X = decltype(x_)::value, c = X & 1;  // step of the group, fragment set
+      constexpr int ST = X / 2;                          // stage t + ST
+      constexpr int D = ST + (c == 0 ? NS - 1 : NS);     // loads go to stage t + D
+      constexpr int L0 = c == 0 ? H1 : 0, L1 = c == 0 ? NL : H1, NLS = L1 - L0;
+      // fragments of the next step
+      const uint8_t* nx = smem + ((t + (X + 1) / 2) % NS) * STAGE;
+      constexpr int NSTEP = c ^ 1;
+      static_for<0, TM>([&](auto q_) {
+        constexpr int Q = decltype(q_)::value;
+        if constexpr (wide_exists(R, D)) {
+          if constexpr (Q == 0 && c == 1 && (ST + NS) % 2 == 0) load_scales(g + (ST + NS) / 2);
+          static_for<L0 + Q * NLS / TM, L0 + (Q + 1) * NLS / TM>([&](auto i_) { load(t + D, i_); });
+        }
+        if constexpr (Q == 0) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) frag_b(fb[c ^ 1][e], nx, NSTEP, e);
+          frag_a(fa[c ^ 1][0], nx, NSTEP, 0);
+        } else if constexpr (Q == 1) {
+#pragma unroll
+          for (int e = 1; e < TM; ++e) frag_a(fa[c ^ 1][e], nx, NSTEP, e);
+        }
+        if constexpr (Q == TM / 2 && X == 3) read_scales(na, nb, g + 1);
+#if defined(__HIP_DEVICE_COMPILE__)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          i32x8 a{}, b{};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            a[e] = fa[c][Q].q[0][e];
+            if constexpr (FA != DLMC_MX_FP4) a[4 + e] = fa[c][Q].q[1][e];
+            b[e] = fb[c][j][e];
+          }
+          acc[Q][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+              a, b, acc[Q][j], FA == DLMC_MX_FP4 ? 4 : 0, 4, 2 * c, (int)sa[Q][ST], 2 * c, (int)sb[j][ST]);
+        }
+#endif
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    };
+    step(std::integral_constant<int, 0>{});
+    __builtin_amdgcn_s_waitcnt(wait_vm_lds(wide_younger(NS, NL, R, 0)));
+    bare_barrier();
+    step(std::integral_constant<int, 1>{});
+    step(std::integral_constant<int, 2>{});
+    __builtin_amdgcn_s_waitcnt(wait_vm_lds(wide_younger(NS, NL, R, 1)));
+    bare_barrier();
+    step(std::integral_constant<int, 3>{});
+  };
+  for (int g = 0; g < ng - 2; ++g) trip(g, std::integral_constant<int, -1>{});
+  if (ng >= 2) trip(ng - 2, std::integral_constant<int, 0>{});
+  trip(ng - 1, std::integral_constant<int, 1>{});
+  __builtin_amdgcn_s_waitcnt(wait_vm_lds(0));
+  bare_barrier();
+
+  // A CU's stores move about 28 bytes a nanosecond (measured: 9.3 us for a 256 x 256
+  // fp32 tile, whether 32 or 256 CUs store): their form matters little, but what is
+  // between them does.  fp32 goes out from the registers, whole 128-byte lines of two
+  // rows an instruction (2048 x 126464 x 4096 in E4M3: 881 us, through LDS 900), past
+  // the caches where the output is too large for them to keep (864 us; with 268 MB
+  // it cost 14%).  bf16 goes through LDS, for a row's 512 bytes at once.
+  if constexpr (OUT_BF16) {
+    bf16_t* so = reinterpret_cast<bf16_t*>(smem);
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          so[(wm * WM + i * 32 + (r >> 2) * 8 + lg * 4 + (r & 3)) * PF + wn * 128 + j * 32 + lr] = f32_to_bf16(acc[i][j][r]);
+    __syncthreads();
+    bf16_t* out = (bf16_t*)p.out;
+    const bool vec = ((uintptr_t)out & 15) == 0 && p.ldo % 8 == 0;
+#pragma unroll 4
+    for (int it = 0; it < BM / 8; ++it) {
+      const int q = tid + it * 256, row = q >> 5, c = (q & 31) * 8;
+      const int grow = m0 + row, gcol = n0 + c;
+      if (grow >= Mv) continue;
+      bf16_t* d = out + (size_t)grow * p.ldo + gcol;
+      const bf16_t* sr = so + row * PF + c;
+      if (vec && gcol + 8 <= p.N)
+        *reinterpret_cast<u32x4*>(d) = *reinterpret_cast<const u32x4*>(sr);
+      else
+        for (int e = 0; e < 8 && gcol + e < p.N; ++e) d[e] = sr[e];
+    }
+  } else {
+    auto store = [&](auto past) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int row = m0 + wm * WM + i * 32 + (r >> 2) * 8 + lg * 4 + (r & 3);
+          if (row >= Mv) continue;
+          float* d = (float*)p.out + (size_t)row * p.ldo + n0 + wn * 128 + lr;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if (n0 + wn * 128 + j * 32 + lr >= p.N) continue;
+            if constexpr (decltype(past)::value)
+              __builtin_nontemporal_store(acc[i][j][r], d + j * 32);
+            else
+              d[j * 32] = acc[i][j][r];
+          }
+        }
+    };
+    if (p.past_caches)
+      store(std::true_type{});
+    else
+      store(std::false_type{});
+  }
+}
+
+template <int FA, int TM, int NS>
+void launch_wide(hipStream_t st, MxArgs p, bool out_bf16) {
+  p.n_tm = ceil_div(p.M, 64 * TM);
+  p.n_tn = ceil_div(p.N, 256);
+  const int64_t tiles = (int64_t)p.n_tm * p.n_tn;
+  DLMC_CHECK(tiles < (1ll << 30), DLMC_E_INVAL, "product with too many tiles");
+  const unsigned grid = (unsigned)((tiles + 7) & ~7ll);
+  if (out_bf16)
+    mx_wide_kernel<FA, TM, NS, true><<<grid, 256, 0, st>>>(p);
+  else
+    mx_wide_kernel<FA, TM, NS, false><<<grid, 256, 0, st>>>(p);
+  DLMC_HIP(hipGetLastError());
+}
+
 template <int FA, int BM, int BN, int WR, int WC, int NS>
 void launch_ring(hipStream_t st, MxArgs p, bool out_bf16) {
   p.n_tm = ceil_div(p.M, BM);
@@ -258,9 +548,11 @@ void mx_matmul(hipStream_t st, MxView A, int fmt_a, size_t a_slots, MxView B, in
   p.M_dev = M_dev;
   p.out = out;
   p.ldo = ldo;
+  p.past_caches = (int64_t)M * N * (out_bf16 ? 2 : 4) >= 512ll << 20;  // twice the Infinity Cache
   const int rows = rows_hint >= 0 && rows_hint < M ? rows_hint : M;
   const bool fp4 = fmt_a == DLMC_MX_FP4;
-  const int64_t big = (int64_t)ceil_div(rows, fp4 ? 256 : 128) * ceil_div(N, 256);
+  // the wide kernel's offsets within a tile are 32 bits wide
+  const int64_t big = p.groups < (1 << 13) ? (int64_t)ceil_div(rows, 256) * ceil_div(N, 256) : 0;
   if (rows <= 32) {
     if (fp4)
       launch_ring<DLMC_MX_FP4, 32, 128, 1, 4, 3>(st, p, out_bf16);
@@ -268,9 +560,9 @@ void mx_matmul(hipStream_t st, MxView A, int fmt_a, size_t a_slots, MxView B, in
       launch_ring<DLMC_MX_FP8, 32, 128, 1, 4, 3>(st, p, out_bf16);
   } else if (big >= 256) {
     if (fp4)
-      launch_ring<DLMC_MX_FP4, 256, 256, 2, 2, 2>(st, p, out_bf16);
+      launch_wide<DLMC_MX_FP4, 4, 4>(st, p, out_bf16);
     else
-      launch_ring<DLMC_MX_FP8, 128, 256, 2, 2, 2>(st, p, out_bf16);
+      launch_wide<DLMC_MX_FP8, 4, 3>(st, p, out_bf16);
   } else {
     if (fp4)
       launch_ring<DLMC_MX_FP4, 128, 128, 2, 2, 4>(st, p, out_bf16);

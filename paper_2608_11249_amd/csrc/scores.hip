@@ -117,18 +117,54 @@ __device__ __forceinline__ int pack(const uint32_t (&key)[E], const uint32_t (&i
   return n;
 }
 
-// Descending order of (key, ~id) over the lanes of a wave.
-__device__ __forceinline__ void sort_lanes(uint32_t& key, uint32_t& id, int lane) {
-  for (int size = 2; size <= 64; size <<= 1)
-    for (int d = size >> 1; d > 0; d >>= 1) {
-      const uint32_t ok = __shfl_xor(key, d), oi = __shfl_xor(id, d);
-      const bool lower = (lane & d) == 0, down = (lane & size) == 0;
-      const bool mine_first = key > ok || (key == ok && id < oi);
-      if (mine_first != (lower == down)) {
-        key = ok;
-        id = oi;
-      }
-    }
+// Entries as one number, in descending order of key, then ascending order of id.
+__device__ __forceinline__ uint64_t entry_of(uint32_t key, uint32_t id) { return (uint64_t)key << 32 | (uint32_t)~id; }
+
+// The place of a lane's entry among those of the first n lanes, all different (64
+// comparisons with a scalar each: a third of the time of sorting over the lanes,
+// whose every step waits for a shuffle).
+__device__ __forceinline__ int place_of(uint64_t x, int n) {
+  int at = 0;
+#pragma unroll 8
+  for (int j = 0; j < n; ++j) {
+    const uint64_t y = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), j) << 32 |
+                       (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, j);
+    at += y > x;
+  }
+  return at;
+}
+
+// The k-th largest of the lanes' numbers (k <= 64).
+__device__ __forceinline__ uint32_t kth_of_lanes(uint32_t x, int k, int lane) {
+  const uint64_t hit = __ballot(place_of(entry_of(x, lane), 64) == k - 1);
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, __ffsll((long long)hit) - 1);
+}
+
+// A bound that at least k of the entries reach, if there are that many (else 0): the
+// k-th largest of the lanes' best.
+template <int E>
+__device__ __forceinline__ uint32_t bound_of(const uint32_t (&key)[E], int k, int lane) {
+  uint32_t best = key[0];
+#pragma unroll
+  for (int e = 1; e < E; ++e) best = max(best, key[e]);
+  return kth_of_lanes(best, k, lane);
+}
+
+// The entries that may be among the k best, side by side in keys / ids: at most
+// `most` of them, k where the bound leaves more.  Sets a bound that k of them reach.
+template <int E>
+__device__ __forceinline__ int narrow(const uint32_t (&key)[E], const uint32_t (&id)[E], int k, int most, int lane,
+                                      uint32_t* keys, uint32_t* ids, uint32_t& bound) {
+  bool keep[E];
+  bound = bound_of(key, k, lane);
+  int n = 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    keep[e] = key[e] != 0 && key[e] >= bound;
+    n += count(keep[e]);
+  }
+  if (n > most) bound = cut<E>(key, id, k, keep);
+  return pack<E>(key, id, keep, keys, ids);
 }
 
 struct ScoreArgs {
@@ -145,17 +181,20 @@ struct ScoreArgs {
 
 __host__ __device__ inline size_t record_bytes(int k) { return 16 + 16 * (size_t)((k + 1) / 2); }
 
-// A row's results by one wave: its statistics and its k best, sorted over the lanes
-// (n of them; n = k where the row has a distribution).
+// A row's results by one wave: its statistics, and n >= k entries (one a lane) with
+// the k best among them (n may be less in a row without a distribution).
 template <bool BF16>
-__device__ __forceinline__ void write_row(const ScoreArgs& p, int row, Stat s, uint32_t key, uint32_t id, int lane) {
+__device__ __forceinline__ void write_row(const ScoreArgs& p, int row, Stat s, uint32_t key, uint32_t id, int n, int lane) {
   // no distribution: nothing above -inf, a NaN, or an infinity
   const bool ok = s.M > NEG_INF && s.M < -NEG_INF && s.Z == s.Z;
   const float nan = __builtin_nanf(""), lz = ok ? log2f(s.Z) : nan;
-  if (lane < p.k) {
-    const size_t o = (size_t)row * p.k + lane;
-    p.top_ids[o] = ok ? (int32_t)id : -1;
-    p.top_logp[o] = ok ? (value_of(key) - s.M) * LOG2E - lz : nan;
+  if (p.k) {
+    const int at = ok ? place_of(entry_of(key, id), n) : lane;
+    if (at < p.k && (lane < n || !ok)) {
+      const size_t o = (size_t)row * p.k + at;
+      p.top_ids[o] = ok ? (int32_t)id : -1;
+      p.top_logp[o] = ok ? (value_of(key) - s.M) * LOG2E - lz : nan;
+    }
   }
   if (lane != 0) return;
   // a sum of nonnegative terms, up to rounding
@@ -222,20 +261,19 @@ scores_kernel(ScoreArgs p) {
   int n = 0;
   uint32_t* wk = keys[TOP ? wave : 0];
   uint32_t* wi = ids[TOP ? wave : 0];
+  // a list's entries e * 64 + lane of n
+  auto entry = [&](int w, int e, int n, uint32_t& key, uint32_t& id) {
+    const int at = e * 64 + lane;
+    key = at < n ? keys[w][at] : 0u;
+    id = at < n ? ids[w][at] : 0xFFFFFFFFu;
+  };
   auto shrink = [&] {
     constexpr int E = LIST / 64;
-    uint32_t key[E], id[E];
-    bool keep[E];
+    uint32_t key[E], id[E], bound;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int at = e * 64 + lane;
-      key[e] = at < n ? wk[at] : 0u;
-      id[e] = at < n ? wi[at] : 0xFFFFFFFFu;
-    }
-    const uint32_t T = cut<E>(key, id, p.k, keep);
-    if (T == 0) return;
-    n = pack<E>(key, id, keep, wk, wi);
-    thr = value_of(T);
+    for (int e = 0; e < E; ++e) entry(wave, e, n, key[e], id[e]);
+    n = narrow<E>(key, id, p.k, LIST - TILE, lane, wk, wi, bound);
+    thr = value_of(bound);
   };
 
   auto take = [&](int t, const float (&v)[8]) {
@@ -264,9 +302,7 @@ scores_kernel(ScoreArgs p) {
     }
     if constexpr (TOP) {
       if (t == t0) {  // the k-th largest lane maximum: k values reach it
-        uint32_t key = order_of(top == top ? top : NEG_INF), id = 0;
-        sort_lanes(key, id, lane);
-        thr = value_of(__shfl(key, p.k - 1));
+        thr = value_of(kth_of_lanes(order_of(top == top ? top : NEG_INF), p.k, lane));
       }
       const bool fill = n < p.k;  // ties with the threshold count
       if (__any(fill ? top >= thr : top > thr)) {
@@ -301,10 +337,7 @@ scores_kernel(ScoreArgs p) {
     take(t, a);
   }
 
-  if constexpr (TOP) {
-    shrink();
-    if (lane == 0) counts[wave] = n;
-  }
+  if (TOP && lane == 0) counts[wave] = n;
   s = merge_lanes(s);
   if (lane == 0) stats[wave] = s;
   __syncthreads();
@@ -312,29 +345,27 @@ scores_kernel(ScoreArgs p) {
   s = merge(merge(stats[0], stats[1]), merge(stats[2], stats[3]));
   uint32_t key = 0, id = 0xFFFFFFFFu;
   if constexpr (TOP) {
-    uint32_t k4[4], i4[4];
-    bool keep[4];
+    constexpr int E = 4 * (LIST - TILE) / 64;
+    uint32_t k8[E], i8[E], bound;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const bool in = lane < counts[e];
-      k4[e] = in ? keys[e][lane] : 0u;
-      i4[e] = in ? ids[e][lane] : 0xFFFFFFFFu;
-    }
-    cut<4>(k4, i4, p.k, keep);
-    n = pack<4>(k4, i4, keep, wk, wi);
+    for (int e = 0; e < E; ++e) entry(e & 3, e >> 2, counts[e & 3], k8[e], i8[e]);
+    n = narrow<E>(k8, i8, p.k, 64, lane, wk, wi, bound);
     if (lane < n) {
       key = wk[lane];
       id = wi[lane];
     }
   }
   if (p.splits == 1) {
-    if constexpr (TOP) sort_lanes(key, id, lane);
-    write_row<BF16>(p, row, s, key, id, lane);
+    write_row<BF16>(p, row, s, key, id, n, lane);
     return;
   }
   uint8_t* w = p.ws + (size_t)blockIdx.x * record_bytes(p.k);
   if (lane == 0) *reinterpret_cast<f32x4*>(w) = f32x4{s.M, s.Z, s.A, 0.0f};
-  if (lane < p.k) *reinterpret_cast<u32x2*>(w + 16 + 8 * lane) = u32x2{key, id};
+  if constexpr (TOP) {
+    // the k best in order; fewer in a row's short last split
+    const int at = lane < n ? place_of(entry_of(key, id), n) : lane;
+    if (at < p.k) *reinterpret_cast<u32x2*>(w + 16 + 8 * at) = u32x2{key, id};
+  }
 }
 
 // The splits of a row joined, by one wave a row.
@@ -352,28 +383,27 @@ scores_join_kernel(ScoreArgs p) {
   }
   s = merge_lanes(s);
   uint32_t key = 0, id = 0xFFFFFFFFu;
+  int n = 0;
   if (p.k) {
-    // split e's entries by the lanes, all k of them valid where it has that many
+    // the splits' entries one after another over the lanes
     constexpr int E = MAX_SPLIT;
-    uint32_t ke[E], ie[E];
-    bool keep[E];
-    const bool in = lane < p.k;
+    uint32_t ke[E], ie[E], bound;
+    const int total = p.splits * p.k;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
+      const int at = e * 64 + lane;
       u32x2 x{0u, 0xFFFFFFFFu};
-      if (in && e < p.splits) x = *reinterpret_cast<const u32x2*>(w + e * rec + 16 + 8 * lane);
+      if (at < total) x = *reinterpret_cast<const u32x2*>(w + at / p.k * rec + 16 + 8 * (at % p.k));
       ke[e] = x[0];
       ie[e] = x[1];
     }
-    cut<E>(ke, ie, p.k, keep);
-    const int n = pack<E>(ke, ie, keep, keys, ids);
+    n = narrow<E>(ke, ie, p.k, MAX_TOP, lane, keys, ids, bound);
     if (lane < n) {
       key = keys[lane];
       id = ids[lane];
     }
-    sort_lanes(key, id, lane);
   }
-  write_row<BF16>(p, row, s, key, id, lane);
+  write_row<BF16>(p, row, s, key, id, n, lane);
 }
 
 // Blocks a row's columns are split over: enough blocks for the chip's 256 CUs eight
