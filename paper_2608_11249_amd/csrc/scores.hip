@@ -7,19 +7,24 @@
 // M, Z, A and rescales them when its M rises.  (The difference comes first: l_i
 // log2 e would overflow in a row masked with the type's lowest value throughout.)
 //
-// Alternatives: each wave keeps a threshold that its k-th best so far reaches, and
-// collects the logits above it in LDS; a full list is cut to its k best, which
-// raises the threshold.  The first threshold is the k-th largest of the 64 lanes'
-// maxima of the wave's first tile.  A wave's tiles come in the order of their
-// columns, so among equal logits the ones collected first have the lowest ids, and
-// later ones equal to the threshold need not be looked at.
+// Alternatives: each wave keeps a threshold that at least k of its logits so far
+// reach, and collects the logits above it in LDS.  The threshold is the k-th largest
+// of the 64 lanes' running maxima (for many alternatives, of the maxima of the lanes'
+// two halves), taken anew with tiles 0, 1, 2, 4, 8, ...: about k logits pass it in the
+// first tile, and fewer and fewer later.  A list that fills up all the same is cut
+// to its k best.  A wave's tiles come in the order of
+// their columns, so among equal logits the ones collected first have the lowest ids,
+// and later ones equal to the threshold need not be looked at.
 #include "kernels.h"
 
 namespace dlmc {
 namespace {
 
 constexpr int TILE = 512;            // columns a wave takes at a time, eight a lane
-constexpr int LIST = 128 + TILE;     // a wave's list: cut above 128, then a whole tile fits
+// Entries of a wave's list before it is cut (a whole tile fits on top): with 96 a CU
+// holds eight blocks, so that 2048 rows are on the chip at once; with more
+// alternatives than 16 it would be cut too often.
+constexpr int FEW_TOP = 16, FEW_LIST = 96, LONG_LIST = 256;
 constexpr int MAX_SPLIT = 32, MAX_TOP = 64;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float NEG_INF = -__builtin_inff();
@@ -134,29 +139,38 @@ __device__ __forceinline__ int place_of(uint64_t x, int n) {
   return at;
 }
 
-// The k-th largest of the lanes' numbers (k <= 64).
-__device__ __forceinline__ uint32_t kth_of_lanes(uint32_t x, int k, int lane) {
-  const uint64_t hit = __ballot(place_of(entry_of(x, lane), 64) == k - 1);
-  return (uint32_t)__builtin_amdgcn_readlane((int)x, __ffsll((long long)hit) - 1);
+// The k-th largest of the lanes' numbers, E in each (k <= 64), bit by bit: mostly
+// scalar work, which other waves' vector work hides.
+template <int E>
+__device__ __forceinline__ uint32_t kth_of_lanes(const uint32_t (&x)[E], int k) {
+  uint32_t T = 0;
+  for (int bit = 31; bit >= 0; --bit) {
+    const uint32_t c = T | 1u << bit;
+    int n = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) n += count(x[e] >= c);
+    if (n >= k) T = c;
+  }
+  return T;
 }
 
 // A bound that at least k of the entries reach, if there are that many (else 0): the
-// k-th largest of the lanes' best.
+// k-th largest of the lanes' best, of both halves' best where there are many entries.
 template <int E>
-__device__ __forceinline__ uint32_t bound_of(const uint32_t (&key)[E], int k, int lane) {
-  uint32_t best = key[0];
+__device__ __forceinline__ uint32_t bound_of(const uint32_t (&key)[E], int k) {
+  uint32_t best[2] = {0u, 0u};
 #pragma unroll
-  for (int e = 1; e < E; ++e) best = max(best, key[e]);
-  return kth_of_lanes(best, k, lane);
+  for (int e = 0; e < E; ++e) best[e % 2] = max(best[e % 2], key[e]);
+  return kth_of_lanes(best, k);
 }
 
 // The entries that may be among the k best, side by side in keys / ids: at most
 // `most` of them, k where the bound leaves more.  Sets a bound that k of them reach.
 template <int E>
-__device__ __forceinline__ int narrow(const uint32_t (&key)[E], const uint32_t (&id)[E], int k, int most, int lane,
+__device__ __forceinline__ int narrow(const uint32_t (&key)[E], const uint32_t (&id)[E], int k, int most,
                                       uint32_t* keys, uint32_t* ids, uint32_t& bound) {
   bool keep[E];
-  bound = bound_of(key, k, lane);
+  bound = bound_of(key, k);
   int n = 0;
 #pragma unroll
   for (int e = 0; e < E; ++e) {
@@ -217,9 +231,11 @@ __device__ __forceinline__ Stat merge_lanes(Stat s) {
   return s;
 }
 
-template <bool BF16, bool TOP>
-__global__ void __launch_bounds__(256)
+template <bool BF16, int CUT>  // CUT: entries before a list is cut, 0 without alternatives
+__global__ void __launch_bounds__(256, CUT == LONG_LIST ? 6 : 8)
 scores_kernel(ScoreArgs p) {
+  constexpr bool TOP = CUT > 0;
+  constexpr int LIST = CUT + TILE;
   __shared__ uint32_t keys[TOP ? 4 : 1][TOP ? LIST : 1], ids[TOP ? 4 : 1][TOP ? LIST : 1];
   __shared__ Stat stats[4];
   __shared__ int counts[4];
@@ -257,7 +273,7 @@ scores_kernel(ScoreArgs p) {
   };
 
   Stat s{NEG_INF, 0.0f, 0.0f};
-  float thr = NEG_INF;
+  float thr = NEG_INF, half[2] = {NEG_INF, NEG_INF};
   int n = 0;
   uint32_t* wk = keys[TOP ? wave : 0];
   uint32_t* wi = ids[TOP ? wave : 0];
@@ -268,18 +284,21 @@ scores_kernel(ScoreArgs p) {
     id = at < n ? ids[w][at] : 0xFFFFFFFFu;
   };
   auto shrink = [&] {
-    constexpr int E = LIST / 64;
+    constexpr int E = (LIST + 63) / 64;
     uint32_t key[E], id[E], bound;
 #pragma unroll
     for (int e = 0; e < E; ++e) entry(wave, e, n, key[e], id[e]);
-    n = narrow<E>(key, id, p.k, LIST - TILE, lane, wk, wi, bound);
+    n = narrow<E>(key, id, p.k, CUT, wk, wi, bound);
     thr = value_of(bound);
   };
 
   auto take = [&](int t, const float (&v)[8]) {
-    float top = v[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) top = fmaxf(top, v[i]);
+    const float lo = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), hi = fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7]));
+    const float top = fmaxf(lo, hi);
+    if constexpr (CUT == LONG_LIST) {
+      half[0] = fmaxf(half[0], lo);
+      half[1] = fmaxf(half[1], hi);
+    }
     if (top > s.M) {
       if (s.M > NEG_INF) {
         const float d = fmaxf((s.M - top) * LOG2E, -1.0e30f), c = __builtin_amdgcn_exp2f(d);
@@ -301,16 +320,27 @@ scores_kernel(ScoreArgs p) {
         if (v[i] != v[i]) s.Z = s.A = v[i];
     }
     if constexpr (TOP) {
-      if (t == t0) {  // the k-th largest lane maximum: k values reach it
-        thr = value_of(kth_of_lanes(order_of(top == top ? top : NEG_INF), p.k, lane));
+      const int seen = t - t0;
+      bool ties = n < p.k;  // logits equal to the threshold count
+      if ((seen & (seen - 1)) == 0) {
+        uint32_t best[2] = {order_of(s.M), 0u};
+        if constexpr (CUT == LONG_LIST) {
+          best[0] = order_of(half[0]);
+          best[1] = order_of(half[1]);
+        }
+        const float up = value_of(kth_of_lanes(best, p.k));
+        if (seen == 0 || up > thr) {
+          thr = up;
+          ties = true;
+        }
       }
-      const bool fill = n < p.k;  // ties with the threshold count
-      if (__any(fill ? top >= thr : top > thr)) {
+      if (__any(ties ? top >= thr : top > thr)) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int c = column(t, i / CH) + i % CH;
-          const bool in = (fill ? v[i] >= thr : v[i] > thr) && c >= 0 && c < p.V;
+          const bool in = (ties ? v[i] >= thr : v[i] > thr) && c >= 0 && c < p.V;
           const uint64_t mask = __ballot(in);
+          if (mask == 0) continue;
           if (in) {
             const int at = n + rank_in(mask);
             wk[at] = order_of(v[i]);
@@ -318,7 +348,7 @@ scores_kernel(ScoreArgs p) {
           }
           n += __popcll(mask);
         }
-        if (n > LIST - TILE) shrink();
+        if (n > CUT) shrink();
       }
     }
   };
@@ -345,11 +375,11 @@ scores_kernel(ScoreArgs p) {
   s = merge(merge(stats[0], stats[1]), merge(stats[2], stats[3]));
   uint32_t key = 0, id = 0xFFFFFFFFu;
   if constexpr (TOP) {
-    constexpr int E = 4 * (LIST - TILE) / 64;
-    uint32_t k8[E], i8[E], bound;
+    constexpr int E = 4 * ((CUT + 63) / 64);
+    uint32_t ke[E], ie[E], bound;
 #pragma unroll
-    for (int e = 0; e < E; ++e) entry(e & 3, e >> 2, counts[e & 3], k8[e], i8[e]);
-    n = narrow<E>(k8, i8, p.k, 64, lane, wk, wi, bound);
+    for (int e = 0; e < E; ++e) entry(e & 3, e >> 2, counts[e & 3], ke[e], ie[e]);
+    n = narrow<E>(ke, ie, p.k, 64, wk, wi, bound);
     if (lane < n) {
       key = wk[lane];
       id = wi[lane];
@@ -368,14 +398,34 @@ scores_kernel(ScoreArgs p) {
   }
 }
 
-// The splits of a row joined, by one wave a row.
+// The splits of a row joined, by one block a row: each wave narrows the entries of
+// eight splits, the first wave what they leave (one wave for all 32 splits took 30 us
+// with 64 alternatives).
 template <bool BF16>
-__global__ void __launch_bounds__(64)
+__global__ void __launch_bounds__(256)
 scores_join_kernel(ScoreArgs p) {
-  __shared__ uint32_t keys[MAX_TOP], ids[MAX_TOP];
-  const int row = blockIdx.x, lane = threadIdx.x;
+  constexpr int EACH = MAX_SPLIT / 4;
+  __shared__ uint32_t keys[4][MAX_TOP], ids[4][MAX_TOP];
+  __shared__ int counts[4];
+  const int row = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const size_t rec = record_bytes(p.k);
   const uint8_t* w = p.ws + (size_t)row * p.splits * rec;
+  if (p.k) {
+    uint32_t ke[EACH], ie[EACH], bound;
+    const int total = min(EACH, p.splits - wave * EACH) * p.k;  // none of a wave past the splits
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      const int at = e * 64 + lane;
+      u32x2 x{0u, 0xFFFFFFFFu};
+      if (at < total) x = *reinterpret_cast<const u32x2*>(w + (wave * EACH + at / p.k) * rec + 16 + 8 * (at % p.k));
+      ke[e] = x[0];
+      ie[e] = x[1];
+    }
+    const int n = total > 0 ? narrow<EACH>(ke, ie, p.k, MAX_TOP, keys[wave], ids[wave], bound) : 0;
+    if (lane == 0) counts[wave] = n;
+    __syncthreads();
+  }
+  if (wave != 0) return;
   Stat s{NEG_INF, 0.0f, 0.0f};
   if (lane < p.splits) {
     const f32x4 v = *reinterpret_cast<const f32x4*>(w + lane * rec);
@@ -385,22 +435,17 @@ scores_join_kernel(ScoreArgs p) {
   uint32_t key = 0, id = 0xFFFFFFFFu;
   int n = 0;
   if (p.k) {
-    // the splits' entries one after another over the lanes
-    constexpr int E = MAX_SPLIT;
-    uint32_t ke[E], ie[E], bound;
-    const int total = p.splits * p.k;
+    uint32_t ke[4], ie[4], bound;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int at = e * 64 + lane;
-      u32x2 x{0u, 0xFFFFFFFFu};
-      if (at < total) x = *reinterpret_cast<const u32x2*>(w + at / p.k * rec + 16 + 8 * (at % p.k));
-      ke[e] = x[0];
-      ie[e] = x[1];
+    for (int e = 0; e < 4; ++e) {
+      const bool in = lane < counts[e];
+      ke[e] = in ? keys[e][lane] : 0u;
+      ie[e] = in ? ids[e][lane] : 0xFFFFFFFFu;
     }
-    n = narrow<E>(ke, ie, p.k, MAX_TOP, lane, keys, ids, bound);
+    n = narrow<4>(ke, ie, p.k, MAX_TOP, keys[0], ids[0], bound);
     if (lane < n) {
-      key = keys[lane];
-      id = ids[lane];
+      key = keys[0][lane];
+      id = ids[0][lane];
     }
   }
   write_row<BF16>(p, row, s, key, id, n, lane);
@@ -426,17 +471,17 @@ void token_scores(hipStream_t st, const void* logits, bool bf16, size_t ld, int 
   DLMC_CHECK(n_top >= 0 && n_top <= MAX_TOP && n_top <= V, DLMC_E_INVAL, "alternatives a row");
   ScoreArgs p{logits, ld, n_rows, V, splits_of(n_rows, V), n_top, tokens, logp, entropy, top_ids, top_logp, (uint8_t*)ws};
   const unsigned grid = (unsigned)n_rows * p.splits;
-  if (bf16) {
-    if (n_top) scores_kernel<true, true><<<grid, 256, 0, st>>>(p);
-    else scores_kernel<true, false><<<grid, 256, 0, st>>>(p);
-  } else {
-    if (n_top) scores_kernel<false, true><<<grid, 256, 0, st>>>(p);
-    else scores_kernel<false, false><<<grid, 256, 0, st>>>(p);
-  }
+  auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(p); };
+  if (n_top == 0)
+    bf16 ? go(scores_kernel<true, 0>) : go(scores_kernel<false, 0>);
+  else if (n_top <= FEW_TOP)
+    bf16 ? go(scores_kernel<true, FEW_LIST>) : go(scores_kernel<false, FEW_LIST>);
+  else
+    bf16 ? go(scores_kernel<true, LONG_LIST>) : go(scores_kernel<false, LONG_LIST>);
   DLMC_HIP(hipGetLastError());
   if (p.splits > 1) {
-    if (bf16) scores_join_kernel<true><<<n_rows, 64, 0, st>>>(p);
-    else scores_join_kernel<false><<<n_rows, 64, 0, st>>>(p);
+    if (bf16) scores_join_kernel<true><<<n_rows, 256, 0, st>>>(p);
+    else scores_join_kernel<false><<<n_rows, 256, 0, st>>>(p);
     DLMC_HIP(hipGetLastError());
   }
 }
