@@ -52,6 +52,11 @@ typedef int32_t dlmc_status;
 #define DLMC_DTYPE_F32 0  /* fp32 weights, activations and accumulation */
 #define DLMC_DTYPE_BF16 1 /* bf16 weights and GEMM inputs, fp32 accumulate,
                              fp32 residual stream, norms, softmax, logits */
+/* the same with the LM head in block-scaled values (see DLMC_MX_FP4): its weights
+ * are held in E2M1, a bit over a quarter of their bf16 bytes, and multiplied by
+ * final-norm rows in E4M3, for fp32 logits.  A model of its own: it decodes no
+ * container of the bf16 model's, nor that its. */
+#define DLMC_DTYPE_BF16_MX4HEAD 2
 
 /* Shape of the masked diffusion LM (Definition 3).  vocab = |Sigma|; the
  * input-only [MASK] token id is vocab.  Weights are random: tensor entries
@@ -60,7 +65,7 @@ typedef int32_t dlmc_status;
 typedef struct dlmc_model_config {
   uint32_t struct_size; /* sizeof(dlmc_model_config) */
   int32_t n_layers;     /* >= 0 */
-  int32_t d_model;      /* multiple of 128 (bf16) or 16 (f32) */
+  int32_t d_model;      /* multiple of 128 (bf16, either head) or 16 (f32) */
   int32_t n_heads;      /* d_model / n_heads in {64, 128} (bf16), <= 128 (f32) */
   int32_t d_ffn;        /* multiple of 64 (bf16) or 16 (f32) */
   int32_t vocab;        /* |Sigma| >= 2; 2^cdf_bits must exceed it */
@@ -274,7 +279,7 @@ dlmc_status dlmc_test_inject_nonfinite(dlmc_model* model, int32_t on);
  * models).  With many masked rows, the head writes only each row's entropy
  * statistics (Schedules, item 3) and the logits of the rows committed in the
  * pass are computed after the selection, which gives the same bits as storing
- * them all.  mode 0 (default): decided per pass by estimated cost; 1: always
+ * them all (a head in E2M1 always stores them).  mode 0 (default): decided per pass by estimated cost; 1: always
  * deferred; 2: never.  Payloads do not depend on the mode.  E_INVAL for
  * another mode. */
 dlmc_status dlmc_test_head_logits(dlmc_model* model, int32_t mode);
@@ -420,7 +425,8 @@ dlmc_status dlmc_token_scores_ws(const dlmc_model* model, int32_t n_rows, int32_
  * host scores[0..T) (two extra forward passes, T <= max_chunk). */
 dlmc_status dlmc_context_scores(dlmc_model* model, const int32_t* tokens, int32_t T, float* scores);
 /* Copy weight tensor `tensor_id` (ids as in dlmc_model_create) to host dst in
- * its canonical [out, in] layout: bf16 bit patterns (uint16) or fp32. */
+ * its canonical [out, in] layout: bf16 bit patterns (uint16) or fp32; of a head held
+ * in E2M1 the values that it stands for, which bf16 holds exactly. */
 dlmc_status dlmc_weight_copy(dlmc_model* model, int32_t tensor_id, void* dst, uint64_t bytes);
 
 /* Stage timing for benchmarks: every launch of a stage whose bit is set in

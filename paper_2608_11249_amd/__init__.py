@@ -23,7 +23,7 @@ HEADER = os.path.join(os.path.dirname(HERE), "include", "dlmc.h")
 
 FFN = {"gelu": 0, "swiglu": 1}
 NORM = {"layernorm": 0, "rmsnorm": 1}
-DTYPE = {"f32": 0, "bf16": 1}
+DTYPE = {"f32": 0, "bf16": 1, "bf16-mx4head": 2}  # bf16-mx4head: the LM head in E2M1
 MX_FORMAT = {"fp4": 0, "fp8": 1}  # E2M1, E4M3
 FLAG_CRC = 1
 STAGES = ["embed", "norm", "qkv", "attn", "oproj", "ffn_in", "ffn_out", "head", "entropy",
@@ -712,7 +712,7 @@ class Model:
 
     def weight(self, tensor_id: int, rows: int, cols: int) -> np.ndarray:
         """A weight tensor in canonical [out, in] layout (uint16 bf16 bits or float32)."""
-        dt = np.uint16 if self.shape.dtype == "bf16" else np.float32
+        dt = np.float32 if self.shape.dtype == "f32" else np.uint16
         out = np.empty((rows, cols), dtype=dt)
         _check(lib().dlmc_weight_copy(self.handle, tensor_id, _ptr(out), out.nbytes))
         return out

@@ -399,6 +399,13 @@ dlmc_status dlmc_weight_copy(dlmc_model* m, int32_t tensor_id, void* dst, uint64
     const size_t row_bytes = (size_t)cols * m->esz;
     DLMC_CHECK(bytes == (size_t)rows * row_bytes, DLMC_E_INVAL, "destination size mismatch");
     DLMC_HIP(hipStreamSynchronize(m->stream));
+    if (tensor_id == 2 && m->mx_head) {  // the values that the codes stand for, exact in bf16
+      void* const values = m->ensure_ws((size_t)bytes);
+      mx_dequantize(m->stream, m->mx_w, DLMC_MX_FP4, rows, cols, values, true, (size_t)cols);
+      DLMC_HIP(hipStreamSynchronize(m->stream));
+      DLMC_HIP(hipMemcpy(dst, values, (size_t)bytes, hipMemcpyDeviceToHost));
+      return;
+    }
     for (int r = 0; r < rows; ++r) {
       int dr = r;
       if (map == MAP_QK_PAIRS) {

@@ -184,13 +184,14 @@ static void validate(const dlmc_model_config& c) {
   DLMC_CHECK(c.d_model % c.n_heads == 0, DLMC_E_INVAL, "d_model must be a multiple of n_heads");
   DLMC_CHECK(c.ffn_kind == DLMC_FFN_GELU || c.ffn_kind == DLMC_FFN_SWIGLU, DLMC_E_INVAL, "ffn_kind");
   DLMC_CHECK(c.norm_kind == DLMC_NORM_LAYER || c.norm_kind == DLMC_NORM_RMS, DLMC_E_INVAL, "norm_kind");
-  DLMC_CHECK(c.dtype == DLMC_DTYPE_F32 || c.dtype == DLMC_DTYPE_BF16, DLMC_E_INVAL, "dtype");
+  DLMC_CHECK(c.dtype == DLMC_DTYPE_F32 || c.dtype == DLMC_DTYPE_BF16 || c.dtype == DLMC_DTYPE_BF16_MX4HEAD,
+             DLMC_E_INVAL, "dtype");
   DLMC_CHECK(c.max_chunk >= 1 && c.max_chunk <= 8192, DLMC_E_INVAL, "max_chunk must be in 1..8192");
   DLMC_CHECK(c.max_batch >= 1 && (int64_t)c.max_batch * c.max_chunk <= (1 << 20), DLMC_E_INVAL,
              "max_batch * max_chunk must be in 1..2^20");
   DLMC_CHECK(c.d_model <= 8192, DLMC_E_INVAL, "d_model above 8192");
   const int dh = c.d_model / c.n_heads;
-  if (c.dtype == DLMC_DTYPE_BF16) {
+  if (c.dtype != DLMC_DTYPE_F32) {
     DLMC_CHECK(c.d_model % 128 == 0 && c.d_ffn % 64 == 0, DLMC_E_INVAL,
                "bf16 model needs d_model a multiple of 128 and d_ffn a multiple of 64");
     DLMC_CHECK(dh == 64 || dh == 128, DLMC_E_INVAL, "bf16 model needs head dim 64 or 128");
@@ -218,11 +219,13 @@ void create_model(dlmc_model* m, const dlmc_model_config& cfg, uint64_t seed, in
   m->stream = m->own_stream;
   m->cfg = cfg;
   m->seed = seed;
-  m->bf16 = cfg.dtype == DLMC_DTYPE_BF16;
+  m->bf16 = cfg.dtype != DLMC_DTYPE_F32;
+  m->mx_head = cfg.dtype == DLMC_DTYPE_BF16_MX4HEAD;
+  m->act = m->bf16 ? DLMC_DTYPE_BF16 : DLMC_DTYPE_F32;
   m->esz = m->bf16 ? 2 : 4;
   const int d = cfg.d_model, F = cfg.d_ffn, V = cfg.vocab, L = cfg.n_layers, H = cfg.n_heads;
   m->dh = d / H;
-  const int dh = m->dh, dt = cfg.dtype;
+  const int dh = m->dh, dt = m->act;
   const bool glu = cfg.ffn_kind == DLMC_FFN_SWIGLU;
   const int nF = glu ? 2 * F : F;
   hipStream_t st = m->stream;
@@ -231,7 +234,14 @@ void create_model(dlmc_model* m, const dlmc_model_config& cfg, uint64_t seed, in
   // not fit fails with E_NOMEM and nothing launched
   // ---- weights
   m->embed = m->dalloc((size_t)(V + 1) * d * m->esz);
-  m->head = m->dalloc((size_t)V * d * m->esz);
+  // an MX head is quantised from its bf16 weights, which are then let go
+  void* const head = m->dalloc((size_t)V * d * m->esz);
+  if (m->mx_head) {
+    m->mx_w.codes = (uint8_t*)m->dalloc(mx_code_bytes(DLMC_MX_FP4, V, d));
+    m->mx_w.scales = (uint8_t*)m->dalloc(mx_scale_bytes(V, d));
+  } else {
+    m->head = head;
+  }
   for (int l = 0; l < L; ++l) {
     dlmc_model::Layer w{};
     w.wqkv = m->dalloc((size_t)3 * d * d * m->esz);
@@ -257,9 +267,14 @@ void create_model(dlmc_model* m, const dlmc_model_config& cfg, uint64_t seed, in
   m->attn = m->dalloc(R * d * m->esz);
   m->ffn = m->dalloc(R * F * m->esz);
   if (!m->bf16) m->tmp = (float*)m->dalloc(R * std::max(3 * d, nF) * 4);
-  m->hm = m->dalloc(R * d * m->esz);
+  if (m->mx_head) {
+    m->mx_h.codes = (uint8_t*)m->dalloc(mx_code_bytes(DLMC_MX_FP8, (int64_t)R, d));
+    m->mx_h.scales = (uint8_t*)m->dalloc(mx_scale_bytes((int64_t)R, d));
+  } else {
+    m->hm = m->dalloc(R * d * m->esz);
+  }
   m->logits = (float*)m->dalloc(R * V * 4);
-  if (m->bf16) m->stats = m->dalloc(R * (size_t)stat_groups(V) * sizeof(RowStat));
+  if (m->fused_stats()) m->stats = m->dalloc(R * (size_t)stat_groups(V) * sizeof(RowStat));
   m->H = (float*)m->dalloc(R * 4);
   m->mx = (float*)m->dalloc(R * 4);
   m->rows = (int32_t*)m->dalloc(R * 4);
@@ -278,7 +293,11 @@ void create_model(dlmc_model* m, const dlmc_model_config& cfg, uint64_t seed, in
 
   // ---- weight generation
   init_weights(st, m->embed, dt, seed, 1, V + 1, d, cfg.embed_exp, MAP_IDENTITY, 0, dh);
-  init_weights(st, m->head, dt, seed, 2, V, d, cfg.head_exp, MAP_IDENTITY, 0, dh);
+  init_weights(st, head, dt, seed, 2, V, d, cfg.head_exp, MAP_IDENTITY, 0, dh);
+  if (m->mx_head) {
+    mx_quantize(st, head, true, (size_t)d, V, d, DLMC_MX_FP4, m->mx_w);
+    m->dfree(head);
+  }
   const RowMap qk_map = m->bf16 ? MAP_QK_PAIRS : MAP_IDENTITY;
   for (int l = 0; l < L; ++l) {
     const dlmc_model::Layer& w = m->layers[l];
@@ -348,7 +367,7 @@ void dlmc_model::forward(const int32_t* st_dev, int B, int T, float* logits_out,
 
   {
     StageTimer t(this, DLMC_STAGE_EMBED, Md * dd * (es + 4.0));
-    dlmc::embed(s, st_dev, this->embed, cfg.dtype, x, M, d, V);
+    dlmc::embed(s, st_dev, this->embed, act, x, M, d, V);
   }
   EpiArgs qkv;
   qkv.q = q;
@@ -378,7 +397,7 @@ void dlmc_model::forward(const int32_t* st_dev, int B, int T, float* logits_out,
     prof_gated = timed_layer >= 0 && layer_index != timed_layer;
     {
       StageTimer t(this, DLMC_STAGE_NORM, norm_bytes);
-      norm_rows(s, x, h, cfg.dtype, M, d, cfg.norm_kind, cfg.norm_eps, nullptr, nullptr);
+      norm_rows(s, x, h, act, M, d, cfg.norm_kind, cfg.norm_eps, nullptr, nullptr);
     }
     if (bf16) {
       {
@@ -425,7 +444,7 @@ void dlmc_model::forward(const int32_t* st_dev, int B, int T, float* logits_out,
     }
     {
       StageTimer t(this, DLMC_STAGE_NORM, norm_bytes);
-      norm_rows(s, x, h, cfg.dtype, M, d, cfg.norm_kind, cfg.norm_eps, nullptr, nullptr);
+      norm_rows(s, x, h, act, M, d, cfg.norm_kind, cfg.norm_eps, nullptr, nullptr);
     }
     if (bf16) {
       EpiArgs f;
@@ -464,10 +483,33 @@ void dlmc_model::forward(const int32_t* st_dev, int B, int T, float* logits_out,
     compact_masked(s, st_dev, B, T, V, rw, nr, chunk_off, chunk_cnt);
   }
   {
-    StageTimer t(this, DLMC_STAGE_NORM, head_rows * dd * (4.0 + es));
-    norm_rows(s, x, hm, cfg.dtype, M, d, cfg.norm_kind, cfg.norm_eps, rw, nr);
+    StageTimer t(this, DLMC_STAGE_NORM, head_rows * dd * (4.0 + (mx_head ? 1.0 + 1.0 / 32 : es)));
+    if (mx_head) {
+      AddNormMx a;
+      a.x = x;
+      a.ldx = (size_t)d;
+      a.gather = rw;
+      a.n_dev = nr;
+      a.q = mx_h;
+      a.slots = mx_slots(max_rows);
+      a.rows = M;
+      a.cols = d;
+      a.norm_kind = cfg.norm_kind;
+      a.fmt = DLMC_MX_FP8;
+      a.eps = cfg.norm_eps;
+      add_norm_mx(s, a);
+    } else {
+      norm_rows(s, x, hm, act, M, d, cfg.norm_kind, cfg.norm_eps, rw, nr);
+    }
   }
-  if (inject_nan) poison_head_input(s, hm, bf16 ? 1 : 0, nr);
+  // (the last byte of an fp32 NaN is E4M3's NaN)
+  if (inject_nan) poison_head_input(s, mx_head ? mx_h.codes : hm, fused_stats() ? 1 : 0, nr);
+  if (mx_head) {
+    StageTimer t(this, DLMC_STAGE_HEAD, 2.0 * head_rows * V * dd);
+    mx_matmul(s, mx_h, DLMC_MX_FP8, mx_slots(max_rows), mx_w, M, V, d, nr, lg, false, (size_t)V,
+              rows_hint >= 0 ? (int)rows_hint : -1);
+    return;
+  }
   // Deferred logits: when writing the fp32 logits of every masked row would
   // take longer than a second read of the head's weights for the committed
   // rows (about 6 TB/s for the stores, 5 TB/s for the weights, 1 PFLOP/s),
@@ -510,7 +552,7 @@ void dlmc_model::selected_logits(int B, int m_max) {
 }
 
 void dlmc_model::row_stats(int n_max) {
-  if (bf16)
+  if (fused_stats())
     entropy_merge(stream, stats, stat_groups(cfg.vocab), cfg.vocab, n_max, n_rows, H, mx);
   else
     entropy_rows(stream, logits, n_max, n_rows, cfg.vocab, H, mx);

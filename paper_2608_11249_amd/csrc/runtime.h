@@ -17,6 +17,8 @@ struct dlmc_model {
   hipStream_t own_stream = nullptr;  // library-created stream
   size_t esz = 2;                    // bytes per weight / GEMM-input element
   bool bf16 = true;
+  bool mx_head = false;  // DLMC_DTYPE_BF16_MX4HEAD
+  int act = 0;           // DLMC_DTYPE_* of activations and of every weight but an MX head
   int dh = 0;
   std::vector<void*> allocs;
 
@@ -25,6 +27,7 @@ struct dlmc_model {
   // interleaved for bf16 SwiGLU), FFN out [d, F]; head [V, d]
   void* embed = nullptr;
   void* head = nullptr;
+  dlmc::MxView mx_w;  // MX head: the head [V, d] in E2M1 (then head is NULL)
   struct Layer {
     void *wqkv, *wo, *win, *wout;
   };
@@ -38,6 +41,7 @@ struct dlmc_model {
   void *h = nullptr, *q = nullptr, *k = nullptr, *vt = nullptr, *attn = nullptr, *ffn = nullptr;
   float* tmp = nullptr;  // fp32 model only: [rows, max(3d, 2F)]
   void* hm = nullptr;    // final-norm rows of masked positions [rows, d]
+  dlmc::MxView mx_h;     // MX head: those rows in E4M3 (then hm is NULL)
   float* logits = nullptr;  // [rows, V]
   void* stats = nullptr;    // bf16 head: softmax statistics per 128-column group [rows, G]
   float *H = nullptr, *mx = nullptr;
@@ -117,7 +121,8 @@ struct dlmc_model {
   void context_scores(const int32_t* tokens, int T, std::vector<float>& score);
   // entropy (bits) and max of the first n_rows[0] (at most n_max) head rows of
   // the last forward into H / mx: merged from the head's group statistics
-  // (bf16), or from the stored logits (fp32); both give the same bits
+  // (bf16 head), or from the stored logits (fp32, MX head); both give the same bits
+  bool fused_stats() const { return bf16 && !mx_head; }
   void row_stats(int n_max);
   // after a deferred head: the logits of the committed rows (sel_row /
   // n_sel, B chunks of m_max slots) into logits, in slot order

@@ -334,7 +334,7 @@ int dlmc_session::step(uint64_t* coded) {
       m->forward(m->state, B, T, nullptr, nullptr, nullptr, masked);
     }
     {
-      StageTimer t(m, DLMC_STAGE_ENTROPY, m->bf16 ? (double)masked * stat_groups(V) * sizeof(RowStat)
+      StageTimer t(m, DLMC_STAGE_ENTROPY, m->fused_stats() ? (double)masked * stat_groups(V) * sizeof(RowStat)
                                                   : (double)masked * V * 4.0);
       m->row_stats(B * T);
     }
@@ -368,7 +368,7 @@ int dlmc_session::step(uint64_t* coded) {
     m->forward(m->state, B, T, nullptr, nullptr, nullptr, r, true);
     {
       // row statistics (the maximum feeds the CDF) at the committed rows only
-      StageTimer t(m, DLMC_STAGE_ENTROPY, m->bf16 ? (double)r * stat_groups(V) * sizeof(RowStat)
+      StageTimer t(m, DLMC_STAGE_ENTROPY, m->fused_stats() ? (double)r * stat_groups(V) * sizeof(RowStat)
                                                   : (double)r * V * 4.0);
       m->row_stats(B * T);
     }

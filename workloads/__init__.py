@@ -48,7 +48,7 @@ class ModelShape:
     vocab: int
     ffn: str            # "gelu" | "swiglu"
     norm: str           # "layernorm" | "rmsnorm"
-    dtype: str          # "f32" | "bf16"
+    dtype: str          # "f32" | "bf16" | "bf16-mx4head"
     rope_theta: float = 10000.0
     norm_eps: float = 1e-5
     embed_exp: int = 0
