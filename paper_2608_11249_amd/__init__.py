@@ -10,7 +10,6 @@ streams to the stage hooks.
 from __future__ import annotations
 
 import ctypes
-import dataclasses
 import os
 import re
 from typing import Callable, Optional, Sequence
@@ -170,35 +169,75 @@ def _refuse(why: str):
     raise DlmcError(-1, lib().dlmc_status_string(-1).decode(), why)
 
 
-@dataclasses.dataclass
 class MXMatrix:
     """A matrix [rows, cols] held with block scales (include/dlmc.h gives the
     layout): torch uint8 tensors codes [rows, pitch] and scales [groups, slots, 8]
-    on the GPU; fmt "fp4" (E2M1) or "fp8" (E4M3)."""
-    codes: object
-    scales: object
-    fmt: str
-    rows: int
-    cols: int
+    on one GPU; fmt "fp4" (E2M1) or "fp8" (E4M3)."""
 
-    def shapes(self):
-        """The shapes of codes and scales."""
-        groups = -(-self.cols // 256)
-        return ((self.rows, groups * (128 if self.fmt == "fp4" else 256)), (groups, -(-self.rows // 32) * 32, 8))
+    __slots__ = ("fmt", "rows", "cols", "device", "_codes", "_scales", "_both", "_ptrs")
+
+    def __init__(self, codes, scales, fmt: str, rows: int, cols: int):
+        shapes = MXMatrix._shapes(fmt, rows, cols)
+        for t, shape in zip((codes, scales), shapes):
+            if not _torch().is_tensor(t) or t.shape != shape or t.element_size() != 1 or not t.is_contiguous():
+                _refuse(f"codes or scales do not fit {rows} x {cols} in {fmt}")
+        self.fmt, self.rows, self.cols, self.device = fmt, rows, cols, codes.get_device()
+        if scales.get_device() != self.device:
+            _refuse("codes and scales must be on one GPU")
+        self._codes, self._scales, self._both = codes, scales, None
+        self._ptrs = codes.data_ptr(), scales.data_ptr()
+
+    @staticmethod
+    def _shapes(fmt: str, rows: int, cols: int):
+        if fmt not in MX_FORMAT:
+            _refuse(f"format must be fp4 or fp8, not {fmt!r}")
+        if rows < 0 or not 1 <= cols <= 1 << 24:
+            _refuse(f"no matrix of {rows} x {cols} values is held")
+        groups = (cols + 255) >> 8
+        return (rows, groups << (7 if fmt == "fp4" else 8)), (groups, (rows + 31) & -32, 8)
 
     @staticmethod
     def like(t, fmt: str, rows: int, cols: int) -> "MXMatrix":
-        """One to be filled, on the device of tensor t."""
-        q = MXMatrix(None, None, fmt, rows, cols)
-        codes, scales = q.shapes()
-        u8 = _torch().uint8
-        q.codes, q.scales = t.new_empty(codes, dtype=u8), t.new_empty(scales, dtype=u8)
+        """One to be filled, on the device of tensor t (both arrays in one allocation:
+        an allocation is a fifth of what a short call costs the host)."""
+        (n, pitch), (groups, slots, _) = MXMatrix._shapes(fmt, rows, cols)
+        q = MXMatrix.__new__(MXMatrix)
+        size = (n * pitch + 255) & -256
+        both = t.new_empty(size + groups * slots * 8, dtype=_torch().uint8)
+        q.fmt, q.rows, q.cols, q.device = fmt, rows, cols, both.get_device()
+        q._codes = q._scales = None
+        q._both = both
+        at = both.data_ptr()
+        q._ptrs = at, at + size
         return q
 
     @staticmethod
     def empty(fmt: str, rows: int, cols: int, device) -> "MXMatrix":
         """One to be filled, on `device`."""
         return MXMatrix.like(_torch().empty(0, device=device), fmt, rows, cols)
+
+    def _part(self, which: int):
+        shape = MXMatrix._shapes(self.fmt, self.rows, self.cols)[which]
+        n = 1
+        for e in shape:
+            n *= e
+        at = self._ptrs[which] - self._ptrs[0] if n else 0
+        return self._both[at: at + n].view(shape)
+
+    def _new(self, dtype, rows: int, cols: int):
+        return (self._codes if self._both is None else self._both).new_empty((rows, cols), dtype=dtype)
+
+    @property
+    def codes(self):
+        if self._codes is None:
+            self._codes = self._part(0)
+        return self._codes
+
+    @property
+    def scales(self):
+        if self._scales is None:
+            self._scales = self._part(1)
+        return self._scales
 
 
 _torch_module = _types = _raw = None
@@ -578,23 +617,13 @@ class Model:
         self._here(t, what)
         return t.contiguous()
 
-    def _held(self, q, what: str, fmt: Optional[str] = None):
-        """(codes, scales) pointers of an MXMatrix on this GPU whose arrays fit it."""
-        if not isinstance(q, MXMatrix) or q.fmt not in MX_FORMAT or q.rows < 0 or not 1 <= q.cols <= 1 << 24:
+    def _held(self, q, what: str):
+        """(codes, scales) pointers of an MXMatrix on this GPU."""
+        if not isinstance(q, MXMatrix):
             _refuse(f"{what} must be an MXMatrix")
-        if fmt is not None and q.fmt != fmt:
-            _refuse(f"{what} must be held in {fmt}, not in {q.fmt}")
-        c, s = q.codes, q.scales
-        if ((c.shape, s.shape) != q.shapes() or c.element_size() != 1 or s.element_size() != 1
-                or not (c.is_contiguous() and s.is_contiguous())):
-            _refuse(f"{what}: codes or scales do not fit {q.rows} x {q.cols} in {q.fmt}")
-        self._here(c, what)
-        self._here(s, what)
-        return c.data_ptr(), s.data_ptr()
-
-    @staticmethod
-    def _format(fmt: str) -> int:
-        return MX_FORMAT[fmt] if fmt in MX_FORMAT else _refuse(f"format must be fp4 or fp8, not {fmt!r}")
+        if q.device != self.device:
+            _refuse(f"{what} must be on the model's GPU (cuda:{self.device})")
+        return q._ptrs
 
     @staticmethod
     def _out_type(dtype) -> int:
@@ -605,12 +634,9 @@ class Model:
         """x [rows, cols] (fp32 or bf16) in E2M1 ("fp4") or E4M3 ("fp8") with a
         power-of-two scale for each 32 columns; nothing saturates."""
         code, ld, ptr = self._rows(x, "x")
-        f = self._format(fmt)
         rows, cols = x.shape
-        if not 1 <= cols <= 1 << 24:
-            _refuse("x must have 1 to 2^24 columns")
         q = MXMatrix.like(x, fmt, rows, cols)
-        self._call(lib().dlmc_mx_quantize, ptr, code, ld, rows, cols, f, q.codes.data_ptr(), q.scales.data_ptr())
+        self._call(lib().dlmc_mx_quantize, ptr, code, ld, rows, cols, MX_FORMAT[fmt], *q._ptrs)
         return q
 
     def mx_dequantize(self, q: MXMatrix, dtype=None):
@@ -619,7 +645,7 @@ class Model:
         dtype = torch.bfloat16 if dtype is None else dtype
         code = self._out_type(dtype)
         codes, scales = self._held(q, "q")
-        out = q.codes.new_empty((q.rows, q.cols), dtype=dtype)
+        out = q._new(dtype, q.rows, q.cols)
         self._call(lib().dlmc_mx_dequantize, codes, scales, MX_FORMAT[q.fmt], q.rows, q.cols, out.data_ptr(), code,
                    q.cols)
         return out
@@ -642,7 +668,6 @@ class Model:
             dcode, ldd, dptr = self._rows(delta, "delta", cols)
             if delta.shape[0] != rows:
                 _refuse(f"delta must have {rows} rows, not {delta.shape[0]}")
-        f = self._format(fmt)
         if gain is not None:
             gain = self._vector(gain, "gain", cols, _torch().float32)
             gptr = gain.data_ptr()
@@ -658,22 +683,24 @@ class Model:
             lds, sptr = cols, r.data_ptr()
         q = MXMatrix.like(x, fmt, rows, cols)
         self._call(lib().dlmc_add_norm_mx, ptr, code, ld, dptr, dcode, ldd, sptr, lds, gptr, kind,
-                   self.shape.norm_eps if eps is None else eps, rows, cols, f, q.codes.data_ptr(),
-                   q.scales.data_ptr())
+                   self.shape.norm_eps if eps is None else eps, rows, cols, MX_FORMAT[fmt],
+                   *q._ptrs)
         return r, q
 
     def mx_matmul(self, a: MXMatrix, b: MXMatrix, out_dtype=None, out=None):
         """a b^T [a.rows, b.rows] of a in either format and b in E2M1, accumulated in
         fp32, as fp32 (the default) or bf16, into `out` if given."""
         ac, asc = self._held(a, "a")
-        bc, bsc = self._held(b, "b", "fp4")
+        bc, bsc = self._held(b, "b")
+        if b.fmt != "fp4":
+            _refuse(f"b must be held in fp4, not in {b.fmt}")
         M, N, K = a.rows, b.rows, a.cols
         if K != b.cols:
             _refuse(f"a has {K} columns, b {b.cols}")
         if out is None:
             dtype = _torch().float32 if out_dtype is None else out_dtype
             code, ldo = self._out_type(dtype), N
-            out = a.codes.new_empty((M, N), dtype=dtype)
+            out = a._new(dtype, M, N)
             optr = out.data_ptr()
         else:
             code, ldo, optr = self._rows(out, "out", N)
