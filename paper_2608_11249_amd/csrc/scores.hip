@@ -8,7 +8,7 @@
 // log2 e would overflow in a row masked with the type's lowest value throughout.)
 //
 // Alternatives: each wave keeps a threshold that at least k of its logits so far
-// reach, and collects the logits above it in LDS.  The threshold is the k-th largest
+// reach, and collects the logits above it in LDS.  The threshold bounds the k-th largest
 // of the 64 lanes' running maxima (for many alternatives, of the maxima of the lanes'
 // two halves), taken anew with tiles 0, 1, 2, 4, 8, ...: about k logits pass it in the
 // first tile, and fewer and fewer later.  A list that fills up all the same is cut
@@ -54,8 +54,15 @@ __device__ __forceinline__ uint32_t order_of(float v) {
   const uint32_t u = __float_as_uint(v + 0.0f);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+constexpr uint32_t LEAST_KEY = 0x007FFFFFu;  // of -inf: numbers below it are no logit's
 __device__ __forceinline__ float value_of(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
+}
+
+// The number before x, a logit above -inf (there is none between -0 and +0).
+__device__ __forceinline__ float before(float x) {
+  const uint32_t k = order_of(x);
+  return value_of(k - (k == 0x80000000u ? 2 : 1));
 }
 
 __device__ __forceinline__ int count(bool p) { return __popcll(__ballot(p)); }
@@ -139,29 +146,37 @@ __device__ __forceinline__ int place_of(uint64_t x, int n) {
   return at;
 }
 
-// The k-th largest of the lanes' numbers, E in each (k <= 64), bit by bit: mostly
-// scalar work, which other waves' vector work hides.
+// A bound that at least k of the lanes' numbers reach, E in each (0 if so many are not
+// above 0): their k-th largest in its upper 20 bits, two bits a step.  (The logit's
+// sign, exponent and eleven bits: what little passes in excess costs less than the
+// 22 steps that the whole number would take bit by bit, each of which waits for a
+// comparison to reach the scalar side: 1.1 us against 0.35.)
 template <int E>
-__device__ __forceinline__ uint32_t kth_of_lanes(const uint32_t (&x)[E], int k) {
+__device__ __forceinline__ uint32_t bound_of_lanes(const uint32_t (&x)[E], int k) {
   uint32_t T = 0;
-  for (int bit = 31; bit >= 0; --bit) {
-    const uint32_t c = T | 1u << bit;
-    int n = 0;
+#pragma unroll 1
+  for (int bit = 30; bit >= 12; bit -= 2) {
+    const uint32_t one = 1u << bit;
+    int n1 = 0, n2 = 0, n3 = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) n += count(x[e] >= c);
-    if (n >= k) T = c;
+    for (int e = 0; e < E; ++e) {
+      n1 += count(x[e] >= T + one);
+      n2 += count(x[e] >= T + 2 * one);
+      n3 += count(x[e] >= T + 3 * one);
+    }
+    T += n3 >= k ? 3 * one : n2 >= k ? 2 * one : n1 >= k ? one : 0u;
   }
   return T;
 }
 
-// A bound that at least k of the entries reach, if there are that many (else 0): the
-// k-th largest of the lanes' best, of both halves' best where there are many entries.
+// A bound that at least k of the entries reach, or 0: of the lanes' best, those of
+// even and of odd entries.
 template <int E>
 __device__ __forceinline__ uint32_t bound_of(const uint32_t (&key)[E], int k) {
   uint32_t best[2] = {0u, 0u};
 #pragma unroll
   for (int e = 0; e < E; ++e) best[e % 2] = max(best[e % 2], key[e]);
-  return kth_of_lanes(best, k);
+  return bound_of_lanes(best, k);
 }
 
 // The entries that may be among the k best, side by side in keys / ids: at most
@@ -289,7 +304,7 @@ scores_kernel(ScoreArgs p) {
 #pragma unroll
     for (int e = 0; e < E; ++e) entry(wave, e, n, key[e], id[e]);
     n = narrow<E>(key, id, p.k, CUT, wk, wi, bound);
-    thr = value_of(bound);
+    thr = value_of(max(bound, LEAST_KEY));
   };
 
   auto take = [&](int t, const float (&v)[8]) {
@@ -322,31 +337,41 @@ scores_kernel(ScoreArgs p) {
     if constexpr (TOP) {
       const int seen = t - t0;
       bool ties = n < p.k;  // logits equal to the threshold count
-      if ((seen & (seen - 1)) == 0) {
+      if (seen == 0 || ((seen & (seen - 1)) == 0 && t1 - t > 2)) {
         uint32_t best[2] = {order_of(s.M), 0u};
         if constexpr (CUT == LONG_LIST) {
           best[0] = order_of(half[0]);
           best[1] = order_of(half[1]);
         }
-        const float up = value_of(kth_of_lanes(best, p.k));
+        const float up = value_of(max(bound_of_lanes(best, p.k), LEAST_KEY));
         if (seen == 0 || up > thr) {
           thr = up;
           ties = true;
         }
       }
-      if (__any(ties ? top >= thr : top > thr)) {
+      auto push = [&](bool in, int i) {
+        const uint64_t mask = __ballot(in);
+        if (mask == 0) return;
+        if (in) {
+          const int at = n + rank_in(mask);
+          wk[at] = order_of(v[i]);
+          wi[at] = (uint32_t)(column(t, i / CH) + i % CH);
+        }
+        n += __popcll(mask);
+      };
+      const bool all = ties && thr == NEG_INF;  // -inf too, but nothing beside the row
+      // where ties count, what lies above the number before the threshold
+      const float above = ties ? before(thr) : thr;
+      if (all || __any(top > above)) {
+        if (all) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int c = column(t, i / CH) + i % CH;
-          const bool in = (ties ? v[i] >= thr : v[i] > thr) && c >= 0 && c < p.V;
-          const uint64_t mask = __ballot(in);
-          if (mask == 0) continue;
-          if (in) {
-            const int at = n + rank_in(mask);
-            wk[at] = order_of(v[i]);
-            wi[at] = (uint32_t)c;
+          for (int i = 0; i < 8; ++i) {
+            const int c = column(t, i / CH) + i % CH;
+            push(v[i] >= thr && c >= 0 && c < p.V, i);
           }
-          n += __popcll(mask);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) push(v[i] > above, i);
         }
         if (n > CUT) shrink();
       }
@@ -398,9 +423,10 @@ scores_kernel(ScoreArgs p) {
   }
 }
 
-// The splits of a row joined, by one block a row: each wave narrows the entries of
-// eight splits, the first wave what they leave (one wave for all 32 splits took 30 us
-// with 64 alternatives).
+// The splits of a row joined, by one block a row.  The first wave takes all their
+// entries where a lane has no more than eight; otherwise each wave narrows those of
+// eight splits, and the first wave what they leave (one wave for 32 splits took
+// 30 us with 64 alternatives).
 template <bool BF16>
 __global__ void __launch_bounds__(256)
 scores_join_kernel(ScoreArgs p) {
@@ -410,45 +436,55 @@ scores_join_kernel(ScoreArgs p) {
   const int row = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const size_t rec = record_bytes(p.k);
   const uint8_t* w = p.ws + (size_t)row * p.splits * rec;
-  if (p.k) {
-    uint32_t ke[EACH], ie[EACH], bound;
-    const int total = min(EACH, p.splits - wave * EACH) * p.k;  // none of a wave past the splits
-#pragma unroll
-    for (int e = 0; e < EACH; ++e) {
-      const int at = e * 64 + lane;
-      u32x2 x{0u, 0xFFFFFFFFu};
-      if (at < total) x = *reinterpret_cast<const u32x2*>(w + (wave * EACH + at / p.k) * rec + 16 + 8 * (at % p.k));
-      ke[e] = x[0];
-      ie[e] = x[1];
-    }
-    const int n = total > 0 ? narrow<EACH>(ke, ie, p.k, MAX_TOP, keys[wave], ids[wave], bound) : 0;
-    if (lane == 0) counts[wave] = n;
-    __syncthreads();
-  }
-  if (wave != 0) return;
+  const bool alone = p.splits * p.k <= EACH * 64;
+  if (alone && wave != 0) return;
   Stat s{NEG_INF, 0.0f, 0.0f};
-  if (lane < p.splits) {
+  if (wave == 0 && lane < p.splits) {
     const f32x4 v = *reinterpret_cast<const f32x4*>(w + lane * rec);
     s = Stat{v[0], v[1], v[2]};
   }
-  s = merge_lanes(s);
   uint32_t key = 0, id = 0xFFFFFFFFu;
   int n = 0;
   if (p.k) {
-    uint32_t ke[4], ie[4], bound;
+    uint32_t ke[EACH], ie[EACH], bound;
+    const int first = alone ? 0 : wave * EACH;
+    const int total = min(alone ? p.splits : EACH, p.splits - first) * p.k;  // none of a wave past the splits
+    // entry e * 64 + lane of the splits' lists one after another
+    int from = lane / p.k, at = lane % p.k;
+    const int step = 64 / p.k, rest = 64 % p.k;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const bool in = lane < counts[e];
-      ke[e] = in ? keys[e][lane] : 0u;
-      ie[e] = in ? ids[e][lane] : 0xFFFFFFFFu;
+    for (int e = 0; e < EACH; ++e) {
+      u32x2 x{0u, 0xFFFFFFFFu};
+      if (e * 64 + lane < total) x = *reinterpret_cast<const u32x2*>(w + (first + from) * rec + 16 + 8 * at);
+      ke[e] = x[0];
+      ie[e] = x[1];
+      from += step;
+      at += rest;
+      if (at >= p.k) {
+        at -= p.k;
+        ++from;
+      }
     }
-    n = narrow<4>(ke, ie, p.k, MAX_TOP, keys[0], ids[0], bound);
+    n = total > 0 ? narrow<EACH>(ke, ie, p.k, MAX_TOP, keys[wave], ids[wave], bound) : 0;
+    if (!alone) {
+      if (lane == 0) counts[wave] = n;
+      __syncthreads();
+      if (wave != 0) return;
+      uint32_t k4[4], i4[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool in = lane < counts[e];
+        k4[e] = in ? keys[e][lane] : 0u;
+        i4[e] = in ? ids[e][lane] : 0xFFFFFFFFu;
+      }
+      n = narrow<4>(k4, i4, p.k, MAX_TOP, keys[0], ids[0], bound);
+    }
     if (lane < n) {
       key = keys[0][lane];
       id = ids[0][lane];
     }
   }
-  write_row<BF16>(p, row, s, key, id, n, lane);
+  write_row<BF16>(p, row, merge_lanes(s), key, id, n, lane);
 }
 
 // Blocks a row's columns are split over: enough blocks for the chip's 256 CUs eight
