@@ -90,19 +90,19 @@ struct MxArgs {
   int past_caches;  // the output is larger than the caches keep
 };
 
-// BM x BN tiles by WR x WC waves, a ring of NS stages of one group (256 columns)
-// of both operands and their scales.
+// BM x BN tiles by WR x WC of four waves (the others only load), a ring of NS stages
+// of one group (256 columns) of both operands and their scales.
 template <int FA, int BM, int BN, int WR, int WC, int NS, bool OUT_BF16>
-__global__ void __launch_bounds__(64 * WR * WC)
+__global__ void __launch_bounds__(256)
 mx_ring_kernel(MxArgs p) {
-  constexpr int NW = WR * WC, WM = BM / WR, WN = BN / WC, TM = WM / 32, TN = WN / 32;
+  constexpr int NW = 4, WM = BM / WR, WN = BN / WC, TM = WM / 32, TN = WN / 32;
   constexpr int AROW = FA == DLMC_MX_FP4 ? 128 : 256, BROW = 128;
-  constexpr int A_B = BM * AROW, B_B = BN * BROW, S_N = ((BM + BN) * 8 + 1023) / 1024;
-  constexpr int S_IN = (S_N + NW - 1) / NW, S_B = S_IN * NW * 1024;
+  constexpr int A_B = BM * AROW, B_B = BN * BROW, S_N = ((BM + BN) * 8 + 1023) / 1024, S_B = S_N * 1024;
+  constexpr int S_IN = (S_N + NW - 1) / NW;  // every wave as many loads, the last window by several
   constexpr int A_IN = A_B / 1024 / NW, B_IN = B_B / 1024 / NW, NL = A_IN + B_IN + S_IN;
   constexpr int STAGE = A_B + B_B + S_B;
   static_assert(A_IN * NW * 1024 == A_B && B_IN * NW * 1024 == B_B, "whole windows per wave");
-  static_assert(NS * STAGE <= 160 * 1024 && (NS - 2) * NL < 64, "LDS / vmcnt field");
+  static_assert(NS >= 2 && NS * STAGE <= 160 * 1024 && (NS - 1) * NL < 64, "LDS / vmcnt field");
   __shared__ __attribute__((aligned(16))) uint8_t smem[NS * STAGE];
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -131,7 +131,7 @@ mx_ring_kernel(MxArgs p) {
   }
 #pragma unroll
   for (int j = 0; j < S_IN; ++j) {  // two rows' scales a lane, A's rows first
-    const int row = ((wave * S_IN + j) * 64 + lane) * 2;
+    const int row = (min(wave * S_IN + j, S_N - 1) * 64 + lane) * 2;
     if (row < BM) {
       s_src[j] = p.as + (size_t)min((size_t)(m0 + row), p.a_slots - 2) * 8;
       s_step[j] = p.a_slots * 8;
@@ -140,15 +140,17 @@ mx_ring_kernel(MxArgs p) {
       s_step[j] = p.b_slots * 8;
     }
   }
-  auto load = [&](int kt) {
+  // load I of group kt
+  auto load = [&](int kt, auto i_) {
+    constexpr int I = decltype(i_)::value;
     uint8_t* st = smem + (kt % NS) * STAGE;
-#pragma unroll
-    for (int j = 0; j < A_IN; ++j) dma16(a_src[j] + (size_t)kt * AROW, st + (wave * A_IN + j) * 1024);
-#pragma unroll
-    for (int j = 0; j < B_IN; ++j) dma16(b_src[j] + (size_t)kt * BROW, st + A_B + (wave * B_IN + j) * 1024);
-#pragma unroll
-    for (int j = 0; j < S_IN; ++j)
-      dma16(s_src[j] + (size_t)kt * s_step[j], st + A_B + B_B + (wave * S_IN + j) * 1024);
+    if constexpr (I < A_IN)
+      dma16(a_src[I] + (size_t)kt * AROW, st + (wave * A_IN + I) * 1024);
+    else if constexpr (I < A_IN + B_IN)
+      dma16(b_src[I - A_IN] + (size_t)kt * BROW, st + A_B + (wave * B_IN + I - A_IN) * 1024);
+    else
+      dma16(s_src[I - A_IN - B_IN] + (size_t)kt * s_step[I - A_IN - B_IN],
+            st + A_B + B_B + min(wave * S_IN + I - A_IN - B_IN, S_N - 1) * 1024);
   };
 
   f32x16 acc[TM][TN];
@@ -159,70 +161,133 @@ mx_ring_kernel(MxArgs p) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
 
-  for (int k = 0; k < NS - 1 && k < ng; ++k) load(k);
-  for (int kt = 0; kt < ng; ++kt) {
-    // this wave's loads of group kt have landed: NS - 2 younger groups may be in
-    // flight, fewer (all waited for) towards the end
-    if (kt + NS - 2 < ng)
-      __builtin_amdgcn_s_waitcnt(wait_vm((NS - 2) * NL));
-    else
-      __builtin_amdgcn_s_waitcnt(wait_vm(0));
-    bare_barrier();  // every wave's have, and group kt - 1 is read
-    if (kt + NS - 1 < ng) load(kt + NS - 1);
+  // a group's fragments, and the lane's scales of its rows: even and odd blocks by
+  // its half, so that bytes 0 and 2 are those of the steps' block
+  struct Frags {
+    i32x4 a[4][TM][FA == DLMC_MX_FP4 ? 1 : 2], b[4][TN];
+    u32x2 sa[TM], sb[TN];
+  };
+  // step S of a group's fragments, with the first also its scales
+  auto read = [&](Frags& f, int kt, auto s_) {
+    constexpr int S = decltype(s_)::value;
     const uint8_t* as = smem + (kt % NS) * STAGE;
     const uint8_t* bs = as + A_B;
     const uint8_t* sc = bs + B_B;
-    // lane's scales of its row: even and odd blocks by its half, so that bytes 0
-    // and 2 are those of the steps' block
-    u32x2 sa[TM], sb[TN];
+    if constexpr (S == 0) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) f.sa[i] = *reinterpret_cast<const u32x2*>(sc + (wm * WM + i * 32 + lr) * 8);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) f.sb[j] = *reinterpret_cast<const u32x2*>(sc + (BM + wn * WN + j * 32 + lr) * 8);
+    }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-      sa[i] = *reinterpret_cast<const u32x2*>(sc + (wm * WM + i * 32 + lr) * 8);
-      sa[i] = u32x2{sa[i][0] >> (8 * lg), sa[i][1] >> (8 * lg)};
+      const int row = wm * WM + i * 32 + lr, x = swizzle<AROW>(row);
+      if constexpr (FA == DLMC_MX_FP4) {
+        f.a[S][i][0] = *reinterpret_cast<const i32x4*>(as + row * AROW + (((2 * S + lg) ^ x) << 4));
+      } else {
+        f.a[S][i][0] = *reinterpret_cast<const i32x4*>(as + row * AROW + (((4 * S + lg) ^ x) << 4));
+        f.a[S][i][1] = *reinterpret_cast<const i32x4*>(as + row * AROW + (((4 * S + 2 + lg) ^ x) << 4));
+      }
     }
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
-      sb[j] = *reinterpret_cast<const u32x2*>(sc + (BM + wn * WN + j * 32 + lr) * 8);
-      sb[j] = u32x2{sb[j][0] >> (8 * lg), sb[j][1] >> (8 * lg)};
+      const int row = wn * WN + j * 32 + lr;
+      f.b[S][j] = *reinterpret_cast<const i32x4*>(bs + row * BROW + (((2 * S + lg) ^ swizzle<BROW>(row)) << 4));
     }
-    auto step = [&](auto s_) {
-      constexpr int S = decltype(s_)::value;
-      i32x8 fa[TM], fb[TN];
+  };
+  auto multiply = [&](const Frags& f, auto s_) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr int S = decltype(s_)::value;
 #pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        const int row = wm * WM + i * 32 + lr;
-        const uint8_t* r = as + row * AROW;
-        const int x = swizzle<AROW>(row);
-        if constexpr (FA == DLMC_MX_FP4) {
-          const i32x4 q = *reinterpret_cast<const i32x4*>(r + (((2 * S + lg) ^ x) << 4));
-          fa[i] = i32x8{q[0], q[1], q[2], q[3], 0, 0, 0, 0};
-        } else {
-          const i32x4 q = *reinterpret_cast<const i32x4*>(r + (((4 * S + lg) ^ x) << 4));
-          const i32x4 t = *reinterpret_cast<const i32x4*>(r + (((4 * S + 2 + lg) ^ x) << 4));
-          fa[i] = i32x8{q[0], q[1], q[2], q[3], t[0], t[1], t[2], t[3]};
-        }
-      }
+    for (int i = 0; i < TM; ++i)
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
-        const int row = wn * WN + j * 32 + lr;
-        const i32x4 q = *reinterpret_cast<const i32x4*>(bs + row * BROW + (((2 * S + lg) ^ swizzle<BROW>(row)) << 4));
-        fb[j] = i32x8{q[0], q[1], q[2], q[3], 0, 0, 0, 0};
+        i32x8 a{}, b{};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          a[e] = f.a[S][i][0][e];
+          if constexpr (FA != DLMC_MX_FP4) a[4 + e] = f.a[S][i][1][e];
+          b[e] = f.b[S][j][e];
+        }
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+            a, b, acc[i][j], FA == DLMC_MX_FP4 ? 4 : 0, 4, 2 * (S & 1), (int)(f.sa[i][S >> 1] >> (8 * lg)),
+            2 * (S & 1), (int)(f.sb[j][S >> 1] >> (8 * lg)));
       }
-#if defined(__HIP_DEVICE_COMPILE__)
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-              fa[i], fb[j], acc[i][j], FA == DLMC_MX_FP4 ? 4 : 0, 4, 2 * (S & 1), (int)sa[i][S >> 1], 2 * (S & 1),
-              (int)sb[j][S >> 1]);
 #endif
-    };
-    step(std::integral_constant<int, 0>{});
-    step(std::integral_constant<int, 1>{});
-    step(std::integral_constant<int, 2>{});
-    step(std::integral_constant<int, 3>{});
+  };
+
+  for (int k = 0; k < NS && k < ng; ++k) static_for<0, NL>([&](auto i_) { load(k, i_); });
+  if (ng >= NS)
+    __builtin_amdgcn_s_waitcnt(wait_vm((NS - 1) * NL));
+  else
+    __builtin_amdgcn_s_waitcnt(wait_vm(0));
+  bare_barrier();
+  Frags f[2];
+  static_for<0, 4>([&](auto s_) { read(f[0], 0, s_); });
+  // Interval kt: this wave's loads of group kt + 1 have landed and its reads of group
+  // kt are done; after the barrier every wave's have and are, so that group kt + NS
+  // may overwrite kt; the fragments of kt + 1 are read under the products of kt.
+  // FULL: groups kt + 1 .. kt + NS exist, and nothing branches.
+  auto interval = [&](int kt, auto set_, auto full_) {
+    constexpr int C = decltype(set_)::value;
+    constexpr bool FULL = decltype(full_)::value;
+    if constexpr (FULL) {
+      __builtin_amdgcn_s_waitcnt(wait_vm((NS - 2) * NL));
+    } else {
+      const int younger = ng - 2 - kt;  // groups whose loads follow those of kt + 1
+      if (younger >= NS - 2) __builtin_amdgcn_s_waitcnt(wait_vm((NS - 2) * NL));
+      static_for<1, NS - 2>([&](auto y_) {
+        constexpr int Y = decltype(y_)::value;
+        if (younger == Y) __builtin_amdgcn_s_waitcnt(wait_vm(Y * NL));
+      });
+      if (younger <= 0) __builtin_amdgcn_s_waitcnt(wait_vm(0));
+    }
+    // the compiler's own wait for the reads of kt goes here, not after those of kt + 1
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      asm volatile("" : "+v"(f[C].sa[i]));
+#pragma unroll
+      for (int S = 0; S < 4; ++S) {
+        asm volatile("" : "+v"(f[C].a[S][i][0]));
+        if constexpr (FA != DLMC_MX_FP4) asm volatile("" : "+v"(f[C].a[S][i][1]));
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      asm volatile("" : "+v"(f[C].sb[j]));
+#pragma unroll
+      for (int S = 0; S < 4; ++S) asm volatile("" : "+v"(f[C].b[S][j]));
+    }
+    bare_barrier();
+    if constexpr (FULL) {
+      // a step's products, then its share of the loads and reads, which are issued
+      // while the products run
+      static_for<0, 4>([&](auto s_) {
+        constexpr int S = decltype(s_)::value;
+        multiply(f[C], s_);
+        read(f[C ^ 1], kt + 1, s_);
+        static_for<S * NL / 4, (S + 1) * NL / 4>([&](auto i_) { load(kt + NS, i_); });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    } else {
+      if (kt + NS < ng) static_for<0, NL>([&](auto i_) { load(kt + NS, i_); });
+      if (kt + 1 < ng) static_for<0, 4>([&](auto s_) { read(f[C ^ 1], kt + 1, s_); });
+      static_for<0, 4>([&](auto s_) { multiply(f[C], s_); });
+    }
+  };
+  using Set0 = std::integral_constant<int, 0>;
+  using Set1 = std::integral_constant<int, 1>;
+  int kt = 0;
+  for (; kt + 1 + NS < ng; kt += 2) {
+    interval(kt, Set0{}, std::true_type{});
+    interval(kt + 1, Set1{}, std::true_type{});
   }
+  for (; kt + 1 < ng; kt += 2) {
+    interval(kt, Set0{}, std::false_type{});
+    interval(kt + 1, Set1{}, std::false_type{});
+  }
+  if (kt < ng) interval(kt, Set0{}, std::false_type{});
+  if (WR * WC < NW && wave >= WR * WC) return;
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -524,9 +589,9 @@ void launch_ring(hipStream_t st, MxArgs p, bool out_bf16) {
   DLMC_CHECK(tiles < (1ll << 30), DLMC_E_INVAL, "product with too many tiles");
   const unsigned grid = (unsigned)((tiles + 7) & ~7ll);
   if (out_bf16)
-    mx_ring_kernel<FA, BM, BN, WR, WC, NS, true><<<grid, 64 * WR * WC, 0, st>>>(p);
+    mx_ring_kernel<FA, BM, BN, WR, WC, NS, true><<<grid, 256, 0, st>>>(p);
   else
-    mx_ring_kernel<FA, BM, BN, WR, WC, NS, false><<<grid, 64 * WR * WC, 0, st>>>(p);
+    mx_ring_kernel<FA, BM, BN, WR, WC, NS, false><<<grid, 256, 0, st>>>(p);
   DLMC_HIP(hipGetLastError());
 }
 
