@@ -21,6 +21,7 @@
 // the launch's other rows.
 #include "kernels.h"
 
+#include <cmath>
 #include <type_traits>
 #include <utility>
 
@@ -90,9 +91,18 @@ struct MxArgs {
   int past_caches;  // the output is larger than the caches keep
 };
 
-// BM x BN tiles by WR x WC of four waves (the others only load), a ring of NS stages
-// of one group (256 columns) of both operands and their scales.
-template <int FA, int BM, int BN, int WR, int WC, int NS, bool OUT_BF16>
+// ---------------------------------------------------------------------------
+// Smaller tiles: BM x BN by WR x WC of four waves (the others only load), a ring of NS
+// stages of one group (256 columns) of both operands and their scales.
+//
+// AHEAD: for launches that leave a CU one tile, where nothing but the wave's own
+// instructions hides a latency: a group's fragments are read into registers under the
+// products of the group before, and loads and reads are issued between the products,
+// each of which waits for the one before (1 x 4096 x 4096 in E2M1 8.5 -> 6.1 us).
+// Without it a CU takes two to four blocks, which hide each other's waits, and the
+// registers of a second set of fragments would cost blocks (2048 x 4096 x 4096 in E4M3
+// on 64 x 128 tiles 36 us, with it 52).
+template <int FA, int BM, int BN, int WR, int WC, int NS, bool AHEAD, bool OUT_BF16>
 __global__ void __launch_bounds__(256)
 mx_ring_kernel(MxArgs p) {
   constexpr int NW = 4, WM = BM / WR, WN = BN / WC, TM = WM / 32, TN = WN / 32;
@@ -216,6 +226,24 @@ mx_ring_kernel(MxArgs p) {
 #endif
   };
 
+  if constexpr (!AHEAD) {
+    for (int k = 0; k < NS - 1 && k < ng; ++k) static_for<0, NL>([&](auto i_) { load(k, i_); });
+    for (int kt = 0; kt < ng; ++kt) {
+      // this wave's loads of group kt have landed: NS - 2 younger groups may be in
+      // flight, fewer (all waited for) towards the end
+      if (kt + NS - 2 < ng)
+        __builtin_amdgcn_s_waitcnt(wait_vm((NS - 2) * NL));
+      else
+        __builtin_amdgcn_s_waitcnt(wait_vm(0));
+      bare_barrier();  // every wave's have, and group kt - 1 is read
+      if (kt + NS - 1 < ng) static_for<0, NL>([&](auto i_) { load(kt + NS - 1, i_); });
+      Frags f;
+      static_for<0, 4>([&](auto s_) {
+        read(f, kt, s_);
+        multiply(f, s_);
+      });
+    }
+  } else {
   for (int k = 0; k < NS && k < ng; ++k) static_for<0, NL>([&](auto i_) { load(k, i_); });
   if (ng >= NS)
     __builtin_amdgcn_s_waitcnt(wait_vm((NS - 1) * NL));
@@ -287,6 +315,7 @@ mx_ring_kernel(MxArgs p) {
     interval(kt + 1, Set1{}, std::false_type{});
   }
   if (kt < ng) interval(kt, Set0{}, std::false_type{});
+  }
   if (WR * WC < NW && wave >= WR * WC) return;
 #pragma unroll
   for (int i = 0; i < TM; ++i)
@@ -529,6 +558,12 @@ mx_wide_kernel(MxArgs p) {
     __syncthreads();
     bf16_t* out = (bf16_t*)p.out;
     const bool vec = ((uintptr_t)out & 15) == 0 && p.ldo % 8 == 0;
+    if (!vec) {  // a row at a time, a column a thread
+#pragma unroll 4
+      for (int row = 0; row < BM; ++row)
+        if (m0 + row < Mv && n0 + tid < p.N) out[(size_t)(m0 + row) * p.ldo + n0 + tid] = so[row * PF + tid];
+      return;
+    }
 #pragma unroll 4
     for (int it = 0; it < BM / 8; ++it) {
       const int q = tid + it * 256, row = q >> 5, c = (q & 31) * 8;
@@ -536,7 +571,7 @@ mx_wide_kernel(MxArgs p) {
       if (grow >= Mv) continue;
       bf16_t* d = out + (size_t)grow * p.ldo + gcol;
       const bf16_t* sr = so + row * PF + c;
-      if (vec && gcol + 8 <= p.N)
+      if (gcol + 8 <= p.N)
         *reinterpret_cast<u32x4*>(d) = *reinterpret_cast<const u32x4*>(sr);
       else
         for (int e = 0; e < 8 && gcol + e < p.N; ++e) d[e] = sr[e];
@@ -581,7 +616,7 @@ void launch_wide(hipStream_t st, MxArgs p, bool out_bf16) {
   DLMC_HIP(hipGetLastError());
 }
 
-template <int FA, int BM, int BN, int WR, int WC, int NS>
+template <int FA, int BM, int BN, int WR, int WC, int NS, bool AHEAD>
 void launch_ring(hipStream_t st, MxArgs p, bool out_bf16) {
   p.n_tm = ceil_div(p.M, BM);
   p.n_tn = ceil_div(p.N, BN);
@@ -589,11 +624,38 @@ void launch_ring(hipStream_t st, MxArgs p, bool out_bf16) {
   DLMC_CHECK(tiles < (1ll << 30), DLMC_E_INVAL, "product with too many tiles");
   const unsigned grid = (unsigned)((tiles + 7) & ~7ll);
   if (out_bf16)
-    mx_ring_kernel<FA, BM, BN, WR, WC, NS, true><<<grid, 256, 0, st>>>(p);
+    mx_ring_kernel<FA, BM, BN, WR, WC, NS, AHEAD, true><<<grid, 256, 0, st>>>(p);
   else
-    mx_ring_kernel<FA, BM, BN, WR, WC, NS, false><<<grid, 256, 0, st>>>(p);
+    mx_ring_kernel<FA, BM, BN, WR, WC, NS, AHEAD, false><<<grid, 256, 0, st>>>(p);
   DLMC_HIP(hipGetLastError());
 }
+
+// Which kernel a product takes: the least of the times that these costs give.  us of
+// a tile beside its groups (start, epilogue), of a group of 256 columns where a CU has
+// one tile, and of a group per tile where it has many (`busy`: the tiles of a CU
+// share the filling and reading of its LDS).  Measured at 1 .. 8192 rows, 768 .. 12288
+// columns and widths of 2304 .. 126464, launches of one kernel each; a choice that is
+// off costs up to a fifth.  Some of what they come from, in us (E2M1 / E4M3):
+//   rows x width x columns    32x64       32x128      64x64       64x128      128x256     256x256
+//       1 x   4096 x  4096    6.1 / 6.8   8.5 / 9.9   7.2 / 8.4    10 / 11     16 / 23     25 / 37
+//      16 x 126464 x  4096     40 / 44     40 / 40     43 / 54     47 / 44     46 / 61     64 / 93
+//     128 x  12288 x  4096     12 / 16     11 / 12    9.7 / 11     12 / 14     17 / 31     26 / 39
+//     777 x   4099 x  1000     11 / 16    9.3 / 10    6.9 / 8.9   7.3 / 8.2    13 / 16     23 / 26
+//    1024 x   4096 x  4096     26 / 36     21 / 24     16 / 25     15 / 18     18 / 33     28 / 40
+//    2048 x   4096 x  4096     48 / 70     40 / 46     32 / 42     30 / 36     22 / 37     31 / 42
+//    2048 x  12288 x  4096                             84 / 114    78 / 102    56 / 80     66 / 87
+// (2048 x 24576 x 4096 in E2M1: 128x256 128, 256x256 112.)
+enum TileKind { RING_32x64, RING_32x128, RING_64x64, RING_64x128, WIDE_128, WIDE_256, TILE_KINDS };
+constexpr int TILE_ROWS[TILE_KINDS] = {32, 32, 64, 64, 128, 256};
+constexpr int TILE_COLS[TILE_KINDS] = {64, 128, 64, 128, 256, 256};
+struct TileCost {
+  float fixed, group, busy;
+};
+constexpr TileCost TILE_COST[2][TILE_KINDS] = {
+    {{0.3f, 0.18f, 0.235f}, {0.3f, 0.375f, 0.42f}, {0.3f, 0.287f, 0.22f}, {0.8f, 0.45f, 0.41f}, {1.9f, 0.73f, 1.16f},
+     {9.7f, 1.15f, 1.55f}},
+    {{0.3f, 0.215f, 0.335f}, {0.4f, 0.47f, 0.465f}, {0.43f, 0.374f, 0.297f}, {1.1f, 0.55f, 0.533f}, {2.6f, 1.7f, 1.667f},
+     {12.0f, 1.94f, 2.05f}}};
 
 }  // namespace
 
@@ -615,24 +677,37 @@ void mx_matmul(hipStream_t st, MxView A, int fmt_a, size_t a_slots, MxView B, in
   p.ldo = ldo;
   p.past_caches = (int64_t)M * N * (out_bf16 ? 2 : 4) >= 512ll << 20;  // twice the Infinity Cache
   const int rows = rows_hint >= 0 && rows_hint < M ? rows_hint : M;
-  const bool fp4 = fmt_a == DLMC_MX_FP4;
-  // the wide kernel's offsets within a tile are 32 bits wide
-  const int64_t big = p.groups < (1 << 13) ? (int64_t)ceil_div(rows, 256) * ceil_div(N, 256) : 0;
-  if (rows <= 32) {
-    if (fp4)
-      launch_ring<DLMC_MX_FP4, 32, 128, 1, 4, 3>(st, p, out_bf16);
-    else
-      launch_ring<DLMC_MX_FP8, 32, 128, 1, 4, 3>(st, p, out_bf16);
-  } else if (big >= 256) {
-    if (fp4)
-      launch_wide<DLMC_MX_FP4, 4, 4>(st, p, out_bf16);
-    else
-      launch_wide<DLMC_MX_FP8, 4, 3>(st, p, out_bf16);
-  } else {
-    if (fp4)
-      launch_ring<DLMC_MX_FP4, 128, 128, 2, 2, 4>(st, p, out_bf16);
-    else
-      launch_ring<DLMC_MX_FP8, 128, 128, 2, 2, 3>(st, p, out_bf16);
+  int best = 0;
+  float least = 0.0f;
+  for (int k = 0; k < TILE_KINDS; ++k) {
+    const TileCost& c = TILE_COST[fmt_a == DLMC_MX_FP4 ? 0 : 1][k];
+    // the wide kernels' offsets within a tile are 32 bits wide
+    if (k >= WIDE_128 && p.groups >= 1 << 13) continue;
+    const float tiles = (float)ceil_div(rows, TILE_ROWS[k]) * (float)ceil_div(N, TILE_COLS[k]) / 256.0f;
+    const float each = k == WIDE_256 ? std::ceil(tiles) : tiles;  // alone on its CU: whole waves
+    const float us = c.fixed * std::max(each, 1.0f) + (float)p.groups * std::max(c.group, each * c.busy);
+    if (k == 0 || us < least) {
+      best = k;
+      least = us;
+    }
+  }
+  if (fmt_a == DLMC_MX_FP4) {
+    switch (best) {
+      case RING_32x64: return launch_ring<DLMC_MX_FP4, 32, 64, 1, 2, 4, true>(st, p, out_bf16);
+      case RING_32x128: return launch_ring<DLMC_MX_FP4, 32, 128, 1, 4, 3, false>(st, p, out_bf16);
+      case RING_64x64: return launch_ring<DLMC_MX_FP4, 64, 64, 2, 2, 2, false>(st, p, out_bf16);
+      case RING_64x128: return launch_ring<DLMC_MX_FP4, 64, 128, 2, 2, 2, false>(st, p, out_bf16);
+      case WIDE_128: return launch_wide<DLMC_MX_FP4, 2, 3>(st, p, out_bf16);
+      default: return launch_wide<DLMC_MX_FP4, 4, 4>(st, p, out_bf16);
+    }
+  }
+  switch (best) {
+    case RING_32x64: return launch_ring<DLMC_MX_FP8, 32, 64, 1, 2, 4, true>(st, p, out_bf16);
+    case RING_32x128: return launch_ring<DLMC_MX_FP8, 32, 128, 1, 4, 3, false>(st, p, out_bf16);
+    case RING_64x64: return launch_ring<DLMC_MX_FP8, 64, 64, 2, 2, 2, false>(st, p, out_bf16);
+    case RING_64x128: return launch_ring<DLMC_MX_FP8, 64, 128, 2, 2, 2, false>(st, p, out_bf16);
+    case WIDE_128: return launch_wide<DLMC_MX_FP8, 2, 2>(st, p, out_bf16);
+    default: return launch_wide<DLMC_MX_FP8, 4, 3>(st, p, out_bf16);
   }
 }
 
