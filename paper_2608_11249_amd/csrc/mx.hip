@@ -238,6 +238,9 @@ void launch_add_norm(hipStream_t st, const AddNormMx& a) {
     add_norm_mx_kernel<FMT, XB, VEC, 4, 4><<<a.rows, 256, 0, st>>>(a);
 }
 
+// Rows of a launch: a grid's threads are counted in 32 bits.
+constexpr int LAUNCH_ROWS = 1 << 23;
+
 inline bool whole16(const void* p, size_t ld, size_t esz) {
   return ((uintptr_t)p & 15) == 0 && ld * esz % 16 == 0;
 }
@@ -247,11 +250,15 @@ inline bool whole16(const void* p, size_t ld, size_t esz) {
 void mx_quantize(hipStream_t st, const void* x, bool bf16, size_t ldx, int rows, int cols, int fmt, MxView q) {
   if (rows <= 0) return;
   const int groups = mx_groups(cols);
-  const dim3 grid((unsigned)ceil_div(rows, 8), (unsigned)ceil_div(groups, Q_GROUPS));
-  const bool vec = cols % 8 == 0 && whole16(x, ldx, bf16 ? 2 : 4);
+  const size_t esz = bf16 ? 2 : 4, pitch = mx_pitch(fmt, cols);
+  const bool vec = cols % 8 == 0 && whole16(x, ldx, esz);
   auto go = [&](auto kernel) {
-    kernel<<<grid, 256, 0, st>>>(x, ldx, rows, cols, q.codes, mx_pitch(fmt, cols), q.scales, mx_slots(rows),
-                                 groups);
+    for (size_t r = 0; r < (size_t)rows; r += LAUNCH_ROWS) {
+      const int n = (int)std::min<size_t>(rows - r, LAUNCH_ROWS);
+      const dim3 grid((unsigned)ceil_div(n, 8), (unsigned)ceil_div(groups, Q_GROUPS));
+      kernel<<<grid, 256, 0, st>>>((const uint8_t*)x + r * ldx * esz, ldx, n, cols, q.codes + r * pitch, pitch,
+                                   q.scales + r * 8, mx_slots(rows), groups);
+    }
   };
   if (fmt == DLMC_MX_FP4) {
     if (bf16) vec ? go(mx_quantize_kernel<DLMC_MX_FP4, true, true>) : go(mx_quantize_kernel<DLMC_MX_FP4, true, false>);
@@ -266,11 +273,15 @@ void mx_quantize(hipStream_t st, const void* x, bool bf16, size_t ldx, int rows,
 void mx_dequantize(hipStream_t st, MxView q, int fmt, int rows, int cols, void* out, bool bf16, size_t ldo) {
   if (rows <= 0) return;
   const int groups = mx_groups(cols);
-  const dim3 grid((unsigned)ceil_div(rows, 8), (unsigned)ceil_div(groups, Q_GROUPS));
-  const bool vec = cols % 8 == 0 && whole16(out, ldo, bf16 ? 2 : 4);
+  const size_t esz = bf16 ? 2 : 4, pitch = mx_pitch(fmt, cols);
+  const bool vec = cols % 8 == 0 && whole16(out, ldo, esz);
   auto go = [&](auto kernel) {
-    kernel<<<grid, 256, 0, st>>>(q.codes, mx_pitch(fmt, cols), q.scales, mx_slots(rows), rows, cols, groups, out,
-                                 ldo);
+    for (size_t r = 0; r < (size_t)rows; r += LAUNCH_ROWS) {
+      const int n = (int)std::min<size_t>(rows - r, LAUNCH_ROWS);
+      const dim3 grid((unsigned)ceil_div(n, 8), (unsigned)ceil_div(groups, Q_GROUPS));
+      kernel<<<grid, 256, 0, st>>>(q.codes + r * pitch, pitch, q.scales + r * 8, mx_slots(rows), n, cols, groups,
+                                   (uint8_t*)out + r * ldo * esz, ldo);
+    }
   };
   if (fmt == DLMC_MX_FP4) {
     if (bf16) vec ? go(mx_dequantize_kernel<DLMC_MX_FP4, true, true>) : go(mx_dequantize_kernel<DLMC_MX_FP4, true, false>);
@@ -287,6 +298,21 @@ void add_norm_mx(hipStream_t st, AddNormMx a) {
   DLMC_CHECK(a.cols >= 1 && a.cols <= ADD_NORM_MAX_COLS, DLMC_E_INVAL, "norm of more columns than a block holds");
   a.pitch_cols = mx_groups(a.cols) * MX_GROUP;
   a.pitch = mx_pitch(a.fmt, a.cols);
+  if (a.rows > LAUNCH_ROWS) {
+    DLMC_CHECK(!a.gather && !a.n_dev, DLMC_E_INVAL, "too many gathered rows");
+    const AddNormMx all = a;
+    const size_t xs = a.x_bf16 ? 2 : 4, ds = a.delta_bf16 ? 2 : 4;
+    for (size_t r = 0; r < (size_t)all.rows; r += LAUNCH_ROWS) {
+      AddNormMx part = all;
+      part.rows = (int)std::min<size_t>(all.rows - r, LAUNCH_ROWS);
+      part.x = (const uint8_t*)all.x + r * all.ldx * xs;
+      if (all.delta) part.delta = (const uint8_t*)all.delta + r * all.ldd * ds;
+      if (all.sum) part.sum = (uint8_t*)all.sum + r * all.lds * xs;
+      part.q = MxView{all.q.codes + r * all.pitch, all.q.scales + r * 8};
+      add_norm_mx(st, part);
+    }
+    return;
+  }
   const bool vec = a.cols % 8 == 0 && whole16(a.x, a.ldx, a.x_bf16 ? 2 : 4) &&
                    (!a.delta || whole16(a.delta, a.ldd, a.delta_bf16 ? 2 : 4)) &&
                    (!a.sum || whole16(a.sum, a.lds, a.x_bf16 ? 2 : 4)) && (!a.gain || ((uintptr_t)a.gain & 15) == 0);

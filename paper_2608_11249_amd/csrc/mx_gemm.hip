@@ -607,7 +607,7 @@ void launch_wide(hipStream_t st, MxArgs p, bool out_bf16) {
   p.n_tm = ceil_div(p.M, 64 * TM);
   p.n_tn = ceil_div(p.N, 256);
   const int64_t tiles = (int64_t)p.n_tm * p.n_tn;
-  DLMC_CHECK(tiles < (1ll << 30), DLMC_E_INVAL, "product with too many tiles");
+  DLMC_CHECK(tiles < (1ll << 24) - 8, DLMC_E_INVAL, "product with too many tiles");  // threads in 32 bits
   const unsigned grid = (unsigned)((tiles + 7) & ~7ll);
   if (out_bf16)
     mx_wide_kernel<FA, TM, NS, true><<<grid, 256, 0, st>>>(p);
@@ -621,7 +621,7 @@ void launch_ring(hipStream_t st, MxArgs p, bool out_bf16) {
   p.n_tm = ceil_div(p.M, BM);
   p.n_tn = ceil_div(p.N, BN);
   const int64_t tiles = (int64_t)p.n_tm * p.n_tn;
-  DLMC_CHECK(tiles < (1ll << 30), DLMC_E_INVAL, "product with too many tiles");
+  DLMC_CHECK(tiles < (1ll << 24) - 8, DLMC_E_INVAL, "product with too many tiles");  // threads in 32 bits
   const unsigned grid = (unsigned)((tiles + 7) & ~7ll);
   if (out_bf16)
     mx_ring_kernel<FA, BM, BN, WR, WC, NS, AHEAD, true><<<grid, 256, 0, st>>>(p);

@@ -505,6 +505,15 @@ void token_scores(hipStream_t st, const void* logits, bool bf16, size_t ld, int 
                   int n_top, float* logp, float* entropy, int32_t* top_ids, float* top_logp, void* ws) {
   if (n_rows <= 0) return;
   DLMC_CHECK(n_top >= 0 && n_top <= MAX_TOP && n_top <= V, DLMC_E_INVAL, "alternatives a row");
+  constexpr int LAUNCH_ROWS = 1 << 23;  // a grid's threads are counted in 32 bits
+  if (n_rows > LAUNCH_ROWS) {           // rows of one block each
+    for (size_t r = 0; r < (size_t)n_rows; r += LAUNCH_ROWS)
+      token_scores(st, (const uint8_t*)logits + r * ld * (bf16 ? 2 : 4), bf16, ld,
+                   (int)std::min<size_t>(n_rows - r, LAUNCH_ROWS), V, tokens ? tokens + r : nullptr, n_top,
+                   tokens ? logp + r : nullptr, entropy + r, n_top ? top_ids + r * n_top : nullptr,
+                   n_top ? top_logp + r * n_top : nullptr, ws);
+    return;
+  }
   ScoreArgs p{logits, ld, n_rows, V, splits_of(n_rows, V), n_top, tokens, logp, entropy, top_ids, top_logp, (uint8_t*)ws};
   const unsigned grid = (unsigned)n_rows * p.splits;
   auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(p); };

@@ -325,6 +325,31 @@ def test_product_past_32_bit_offsets(m):
     assert torch.equal(out[-40:, :500], m.mx_matmul(m.mx_quantize(a[-40:], "fp8"), first, torch.bfloat16))
 
 
+def test_more_rows_than_one_launch_takes(m):
+    """Rows past 2^24: a grid of one block each has more threads than 32 bits count."""
+    n = (1 << 24) + 5
+    log("rows past 2^24", n)
+    x = torch.randn(n, 2, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    last = torch.cat((x[:3], x[(1 << 23) - 2: (1 << 23) + 2], x[-6:]))
+    pick = lambda t: torch.cat((t[:3], t[(1 << 23) - 2: (1 << 23) + 2], t[-6:]))  # noqa: E731
+    for fmt in ("fp8", "fp4"):
+        q = m.mx_quantize(x, fmt)
+        got = m.mx_dequantize(q, torch.float32)
+        assert torch.equal(pick(got), m.mx_dequantize(m.mx_quantize(last, fmt), torch.float32))
+        # off by less than a half step of 2^-4 or 2^-2, whose values all blocks have
+        assert bool(((got - x).abs() <= x.abs().amax(1, keepdim=True) * 0.25).all())
+        del q, got
+    wide = torch.zeros(n, 1100, dtype=torch.bfloat16, device="cuda")  # a block a row
+    wide[:, :2] = x
+    r, q = m.add_norm_mx(wide, wide, fmt="fp4", norm="rmsnorm", eps=1e-5)
+    small = pick(wide)
+    want, p = m.add_norm_mx(small, small, fmt="fp4", norm="rmsnorm", eps=1e-5)
+    assert torch.equal(pick(r), want) and torch.equal(pick(q.codes), p.codes)
+    assert torch.equal(pick(q.scales[:, :n].transpose(0, 1)), p.scales[:, : len(small)].transpose(0, 1))
+    for t in range(0, n, 1 << 22):  # no row was left out
+        assert torch.equal(r[t: t + (1 << 22)], wide[t: t + (1 << 22)] * 2)
+
+
 # ---------------------------------------------------------------- together
 def chain(m, x, d, w, tokens):
     r, q = m.add_norm_mx(x, d, fmt="fp8", norm="rmsnorm", eps=1e-5)

@@ -188,6 +188,24 @@ def test_offsets_past_32_bits():
         check(tail, reference(lg[-3:].float().cpu().numpy(), tok[-3:].cpu().numpy(), 3), V)
 
 
+def test_more_rows_than_one_launch_takes():
+    """Rows past 2^24: a grid of one block each has more threads than 32 bits count."""
+    V, n = 5, (1 << 24) + 3
+    log("rows past 2^24", n)
+    g = torch.Generator(device="cuda").manual_seed(7)
+    lg = torch.randn(n, V, generator=g, device="cuda")
+    tok = torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32)
+    with model(V) as m:
+        lp, h, ids, tlp = m.token_scores(lg, tok, top=2)
+        p = torch.log_softmax(lg.double(), 1) / np.log(2)
+        # five terms: a few half steps of fp32 relative to the sum, and of |log2 p| < 32
+        assert float((lp - p.gather(1, tok.long()[:, None])[:, 0]).abs().max()) < 64 * 2.0 ** -24 * 32
+        assert float((h + (p.exp2() * p).sum(1)).abs().max()) < 64 * 2.0 ** -24 * 32
+        want = torch.sort(lg, dim=1, descending=True, stable=True)[1][:, :2]
+        assert torch.equal(ids, want.int())
+        assert float((tlp - p.gather(1, want)).abs().max()) < 64 * 2.0 ** -24 * 32
+
+
 def test_no_rows_and_refusals():
     V = 300
     lg = torch.randn(4, V, device="cuda")
