@@ -17,6 +17,8 @@
 // and later ones equal to the threshold need not be looked at.
 #include "kernels.h"
 
+#include <type_traits>
+
 namespace dlmc {
 namespace {
 
@@ -210,10 +212,20 @@ struct ScoreArgs {
 
 __host__ __device__ inline size_t record_bytes(int k) { return 16 + 16 * (size_t)((k + 1) / 2); }
 
-// A row's results by one wave: its statistics, and n >= k entries (one a lane) with
+// A row's results by one wave: its statistics, its token t with logit l, and n >= k entries (one a lane) with
 // the k best among them (n may be less in a row without a distribution).
+// The logit of the row's token; 0 without one within the vocabulary.  (Read ahead of
+// the work that leads up to write_row: two loads one after the other.)
 template <bool BF16>
-__device__ __forceinline__ void write_row(const ScoreArgs& p, int row, Stat s, uint32_t key, uint32_t id, int n, int lane) {
+__device__ __forceinline__ float token_logit(const ScoreArgs& p, int row, int& t) {
+  t = p.tokens ? p.tokens[row] : -1;
+  if (t < 0 || t >= p.V) return 0.0f;
+  const size_t at = (size_t)row * p.ld + t;
+  return BF16 ? bf16_to_f32(((const bf16_t*)p.logits)[at]) : ((const float*)p.logits)[at];
+}
+
+__device__ __forceinline__ void write_row(const ScoreArgs& p, int row, Stat s, uint32_t key, uint32_t id, int n, int lane,
+                                          int t, float l) {
   // no distribution: nothing above -inf, a NaN, or an infinity
   const bool ok = s.M > NEG_INF && s.M < -NEG_INF && s.Z == s.Z;
   const float nan = __builtin_nanf(""), lz = ok ? log2f(s.Z) : nan;
@@ -229,24 +241,43 @@ __device__ __forceinline__ void write_row(const ScoreArgs& p, int row, Stat s, u
   // a sum of nonnegative terms, up to rounding
   const float h = lz - s.A / s.Z;
   p.entropy[row] = ok ? (h < 0.0f ? 0.0f : h) : nan;
-  if (p.tokens) {
-    const int t = p.tokens[row];
-    float r = t == -1 ? 0.0f : nan;
-    if (ok && t >= 0 && t < p.V) {
-      const size_t at = (size_t)row * p.ld + t;
-      const float l = BF16 ? bf16_to_f32(((const bf16_t*)p.logits)[at]) : ((const float*)p.logits)[at];
-      r = (l - s.M) * LOG2E - lz;
-    }
-    p.logp[row] = r;
-  }
+  if (p.tokens) p.logp[row] = t == -1 ? 0.0f : ok && t >= 0 && t < p.V ? (l - s.M) * LOG2E - lz : nan;
 }
 
+// A number reduced over the wave's lanes, the same in all of them: within 16 lanes by
+// DPP moves, then the four results (a shuffle would go through LDS, six times in turn).
+template <typename F>
+__device__ __forceinline__ float reduce_lanes(float x, F f) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  auto at = [&](auto ctrl) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  x = f(x, at(std::integral_constant<int, 0xB1>{}));   // lane ^ 1
+  x = f(x, at(std::integral_constant<int, 0x4E>{}));   // lane ^ 2
+  x = f(x, at(std::integral_constant<int, 0x141>{}));  // 7 - lane, of each eight
+  x = f(x, at(std::integral_constant<int, 0x140>{}));  // 15 - lane, of each sixteen
+  auto lane = [&](int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), l)); };
+  x = f(f(lane(0), lane(16)), f(lane(32), lane(48)));
+#endif
+  return x;
+}
+
+// The lanes' statistics joined.  Without a logit above -inf a lane's Z is zero or NaN,
+// and stays so whatever it is scaled with.
 __device__ __forceinline__ Stat merge_lanes(Stat s) {
-  for (int o = 1; o < 64; o <<= 1) s = merge(s, Stat{__shfl_xor(s.M, o), __shfl_xor(s.Z, o), __shfl_xor(s.A, o)});
-  return s;
+  const float M = reduce_lanes(s.M, [](float a, float b) { return fmaxf(a, b); });
+  if (M > NEG_INF) {
+    const float d = fmaxf((s.M - M) * LOG2E, -1.0e30f), c = __builtin_amdgcn_exp2f(d);
+    s.A = c * fmaf(d, s.Z, s.A);
+    s.Z *= c;
+  }
+  auto add = [](float a, float b) { return a + b; };
+  return {M, reduce_lanes(s.Z, add), reduce_lanes(s.A, add)};
 }
 
-template <bool BF16, int CUT>  // CUT: entries before a list is cut, 0 without alternatives
+// ROWS 1: a row, or one of its `splits` parts, by a block's four waves; ROWS 4: a row
+// by each of them.  CUT: entries before a list is cut, 0 without alternatives.
+template <bool BF16, int CUT, int ROWS>
 __global__ void __launch_bounds__(256, CUT == LONG_LIST ? 6 : 8)
 scores_kernel(ScoreArgs p) {
   constexpr bool TOP = CUT > 0;
@@ -255,14 +286,21 @@ scores_kernel(ScoreArgs p) {
   __shared__ Stat stats[4];
   __shared__ int counts[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row = blockIdx.x / p.splits, split = blockIdx.x % p.splits;
+  const int row = ROWS == 4 ? blockIdx.x * 4 + wave : blockIdx.x / p.splits;
+  const int split = ROWS == 4 ? 0 : blockIdx.x % p.splits;
+  if (ROWS == 4 && row >= p.n_rows) return;  // a whole wave; they do not wait for each other
   constexpr int CH = BF16 ? 8 : 4;  // columns of a 16-byte load
   const uint8_t* base = (const uint8_t*)p.logits + (size_t)row * p.ld * (BF16 ? 2 : 4);
   // columns are counted from the 16-byte border at or below the row's start
   const int shift = (int)((uintptr_t)base / (BF16 ? 2 : 4) % CH);
   const int nt = (p.V + shift + TILE - 1) / TILE;
-  const int per = (nt + 4 * p.splits - 1) / (4 * p.splits);
-  const int t0 = (split * 4 + wave) * per, t1 = min(t0 + per, nt);
+  const int per = ROWS == 4 ? nt : (nt + 4 * p.splits - 1) / (4 * p.splits);
+  const int t0 = ROWS == 4 ? 0 : (split * 4 + wave) * per, t1 = min(t0 + per, nt);
+
+  // read by the wave that writes the row, ahead of its logits
+  int tok = -1;
+  float tok_logit = 0.0f;
+  if (ROWS == 4 || (p.splits == 1 && wave == 0)) tok_logit = token_logit<BF16>(p, row, tok);
 
   auto column = [&](int t, int q) {  // first column of the lane's chunk q of tile t
     return t * TILE - shift + (BF16 ? lane * 8 : q * 256 + lane * 4);
@@ -363,15 +401,14 @@ scores_kernel(ScoreArgs p) {
       // where ties count, what lies above the number before the threshold
       const float above = ties ? before(thr) : thr;
       if (all || __any(top > above)) {
-        if (all) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 8; ++i) {
+          bool in = v[i] > above;
+          if (all) {
             const int c = column(t, i / CH) + i % CH;
-            push(v[i] >= thr && c >= 0 && c < p.V, i);
+            in = v[i] >= thr && c >= 0 && c < p.V;
           }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) push(v[i] > above, i);
+          push(in, i);
         }
         if (n > CUT) shrink();
       }
@@ -392,6 +429,23 @@ scores_kernel(ScoreArgs p) {
     take(t, a);
   }
 
+  if constexpr (ROWS == 4) {
+    s = merge_lanes(s);
+    uint32_t key = 0, id = 0xFFFFFFFFu;
+    if constexpr (TOP) {
+      constexpr int E = (CUT + 63) / 64;
+      uint32_t ke[E], ie[E], bound;
+#pragma unroll
+      for (int e = 0; e < E; ++e) entry(wave, e, n, ke[e], ie[e]);
+      if (n > 64) n = narrow<E>(ke, ie, p.k, 64, wk, wi, bound);
+      if (lane < n) {
+        key = wk[lane];
+        id = wi[lane];
+      }
+    }
+    write_row(p, row, s, key, id, n, lane, tok, tok_logit);
+    return;
+  }
   if (TOP && lane == 0) counts[wave] = n;
   s = merge_lanes(s);
   if (lane == 0) stats[wave] = s;
@@ -411,7 +465,7 @@ scores_kernel(ScoreArgs p) {
     }
   }
   if (p.splits == 1) {
-    write_row<BF16>(p, row, s, key, id, n, lane);
+    write_row(p, row, s, key, id, n, lane, tok, tok_logit);
     return;
   }
   uint8_t* w = p.ws + (size_t)blockIdx.x * record_bytes(p.k);
@@ -438,6 +492,8 @@ scores_join_kernel(ScoreArgs p) {
   const uint8_t* w = p.ws + (size_t)row * p.splits * rec;
   const bool alone = p.splits * p.k <= EACH * 64;
   if (alone && wave != 0) return;
+  int tok = -1;
+  const float tok_logit = wave == 0 ? token_logit<BF16>(p, row, tok) : 0.0f;
   Stat s{NEG_INF, 0.0f, 0.0f};
   if (wave == 0 && lane < p.splits) {
     const f32x4 v = *reinterpret_cast<const f32x4*>(w + lane * rec);
@@ -484,20 +540,38 @@ scores_join_kernel(ScoreArgs p) {
       id = ids[0][lane];
     }
   }
-  write_row<BF16>(p, row, merge_lanes(s), key, id, n, lane);
+  write_row(p, row, merge_lanes(s), key, id, n, lane, tok, tok_logit);
+}
+
+// Whether each wave takes a row: where a row is a tile or two, or there are rows for
+// half of the chip's waves; with 512 rows up to ten tiles, which take a wave no longer
+// than a block's waves take to join.  us with 0 / 5 / 20 alternatives, a row a block and
+// a row a wave, fp32:
+//   42115 x   265    52 / 146 / 223     18 /  39 /  55
+//   44113 x  4099   144 / 279 / 368    125 / 172 / 220
+//    4096 x 32768   108 / 128 / 146    105 / 125 / 128
+//    1000 x  4099    11 /  22 /  27    8.7 /  19 /  21
+//     100 x  4099   6.1 /  13 /  15    6.4 /  16 /  19
+//    2000 x  8000    16 /  28 /  34     21 /  35 /  36
+//    1000 x 32768    31 /  49 /  58     54 /  81 /  87
+bool rows_by_waves(int n_rows, int V) {
+  return V <= 2 * TILE || n_rows >= 4096 || (n_rows >= 512 && V <= 10 * TILE);
 }
 
 // Blocks a row's columns are split over: enough blocks for the chip's 256 CUs eight
-// times over, but at least two tiles to a wave.
+// times over, but at least two tiles to a wave, and three blocks, as joining costs a
+// launch (1000 x 32768 with 5 alternatives in two 49 us, unsplit 45; 600 x 126464 in
+// three 86, unsplit 113).
 int splits_of(int n_rows, int V) {
-  const int most = std::max(1, std::min(MAX_SPLIT, V / (8 * TILE)));
-  return std::max(1, std::min(most, 2048 / std::max(n_rows, 1)));
+  if (rows_by_waves(n_rows, V)) return 1;
+  const int s = std::min({2048 / n_rows, ceil_div(V + 7, 8 * TILE), MAX_SPLIT});
+  return s < 3 ? 1 : s;
 }
 
 }  // namespace
 
 size_t token_scores_ws(int n_rows, int V, int n_top) {
-  const int s = splits_of(n_rows, V);
+  const int s = n_rows > 0 ? splits_of(n_rows, V) : 1;
   return s == 1 ? 0 : (size_t)n_rows * s * record_bytes(n_top);
 }
 
@@ -515,14 +589,17 @@ void token_scores(hipStream_t st, const void* logits, bool bf16, size_t ld, int 
     return;
   }
   ScoreArgs p{logits, ld, n_rows, V, splits_of(n_rows, V), n_top, tokens, logp, entropy, top_ids, top_logp, (uint8_t*)ws};
-  const unsigned grid = (unsigned)n_rows * p.splits;
-  auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(p); };
+  const bool wave_rows = rows_by_waves(n_rows, V);
+  const unsigned grid = wave_rows ? (unsigned)ceil_div(n_rows, 4) : (unsigned)n_rows * p.splits;
+  auto go = [&](auto four, auto one) { (wave_rows ? four : one)<<<grid, 256, 0, st>>>(p); };
   if (n_top == 0)
-    bf16 ? go(scores_kernel<true, 0>) : go(scores_kernel<false, 0>);
+    bf16 ? go(scores_kernel<true, 0, 4>, scores_kernel<true, 0, 1>) : go(scores_kernel<false, 0, 4>, scores_kernel<false, 0, 1>);
   else if (n_top <= FEW_TOP)
-    bf16 ? go(scores_kernel<true, FEW_LIST>) : go(scores_kernel<false, FEW_LIST>);
+    bf16 ? go(scores_kernel<true, FEW_LIST, 4>, scores_kernel<true, FEW_LIST, 1>)
+         : go(scores_kernel<false, FEW_LIST, 4>, scores_kernel<false, FEW_LIST, 1>);
   else
-    bf16 ? go(scores_kernel<true, LONG_LIST>) : go(scores_kernel<false, LONG_LIST>);
+    bf16 ? go(scores_kernel<true, LONG_LIST, 4>, scores_kernel<true, LONG_LIST, 1>)
+         : go(scores_kernel<false, LONG_LIST, 4>, scores_kernel<false, LONG_LIST, 1>);
   DLMC_HIP(hipGetLastError());
   if (p.splits > 1) {
     if (bf16) scores_join_kernel<true><<<n_rows, 256, 0, st>>>(p);

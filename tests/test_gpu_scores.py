@@ -72,6 +72,26 @@ def test_many_rows(n, V):
         check(got, reference(lg, tok, 5), V)
 
 
+@pytest.mark.parametrize("n,V", [(3, 1023), (3, 1024), (3, 1025), (511, 5120), (512, 5120), (513, 5121), (682, 9000),
+                                 (683, 9000), (4095, 6000), (4096, 6000), (4099, 6000)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_either_side_of_the_launchs_choices(n, V, dtype):
+    """A row to a wave, to a block, or to several blocks; rows that do not fill a block."""
+    g = torch.Generator(device="cuda").manual_seed(n + V)
+    lg = (torch.randn(n, V, generator=g, device="cuda") * 4).to(getattr(torch, dtype))
+    lg[n // 2, : V - 30] = float("-inf")
+    tok = torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32)
+    some = torch.arange(0, n, max(1, n // 40), device="cuda")
+    some = torch.cat((some, torch.tensor([n // 2, n - 1], device="cuda")))
+    with model(V) as m:
+        for top in (0, 3, 30):
+            log("choices", n, V, dtype, top)
+            got = m.token_scores(lg, tok, top=top)
+            check([t[some] for t in got], reference(lg[some].float().cpu().numpy(), tok[some].cpu().numpy(), top), V)
+            order = torch.sort(lg, dim=1, descending=True, stable=True)[1][:, :top]
+            assert torch.equal(got[2], order.int())
+
+
 @pytest.mark.parametrize("V", [700, 5000, 40001])
 def test_ties_and_orders(V):
     """Equal logits go by id, in rows that rise, fall, hold few values or one; -0 is 0."""
