@@ -164,7 +164,8 @@ void dlmc_model_destroy(dlmc_model* model);
 /* Use `hip_stream` (a hipStream_t) for all device work of this model;
  * DLMC_DEFAULT_STREAM selects the device's default stream (handle 0, e.g. torch's
  * unless another is current), and NULL the library's own stream, which waits
- * for no other: device memory handed to a call on it has to be ready. */
+ * for no other: device memory handed to a call on it has to be ready.  Waits for
+ * the work on the stream used before, unless one of the two is being captured. */
 #define DLMC_DEFAULT_STREAM ((void*)1)
 dlmc_status dlmc_set_stream(dlmc_model* model, void* hip_stream);
 
@@ -347,8 +348,8 @@ dlmc_status dlmc_select_rank_rows(dlmc_model* model, const float* logits, int32_
 /* The calls of this section enqueue their work on the model's stream and return
  * without waiting for it: results are ready once the stream has come that far.
  * They allocate nothing and keep no state between calls, so they may be captured
- * into a HIP graph (once the model's stream is the capturing one), and calls on
- * several streams do not disturb each other.  They leave the calling thread's
+ * into a HIP graph (dlmc_set_stream to or from a capturing stream is allowed, and
+ * does not wait), and calls on several streams do not disturb each other.  They leave the calling thread's
  * current device as it was.  Element types are DLMC_DTYPE_F32 and
  * DLMC_DTYPE_BF16; ld* is the distance of two rows in elements (>= the row's
  * length) and rows need no alignment beyond their elements' own (rows of whole

@@ -58,6 +58,12 @@ struct OnDevice {
   }
 };
 
+bool capturing(hipStream_t s) {
+  hipStreamCaptureStatus now = hipStreamCaptureStatusNone;
+  if (s) DLMC_HIP(hipStreamIsCapturing(s, &now));  // the default stream never is
+  return now != hipStreamCaptureStatusNone;
+}
+
 bool is_bf16(int32_t dtype) {
   DLMC_CHECK(dtype == DLMC_DTYPE_F32 || dtype == DLMC_DTYPE_BF16, DLMC_E_INVAL, "element type must be fp32 or bf16");
   return dtype == DLMC_DTYPE_BF16;
@@ -115,11 +121,14 @@ void dlmc_model_destroy(dlmc_model* model) { delete model; }
 
 dlmc_status dlmc_set_stream(dlmc_model* m, void* hip_stream) {
   return guard([&] {
-    use(m);
-    DLMC_HIP(hipStreamSynchronize(m->stream));
-    m->stream = hip_stream == DLMC_DEFAULT_STREAM ? nullptr
-                : hip_stream                       ? (hipStream_t)hip_stream
-                                                   : m->own_stream;
+    OnDevice on(m);
+    hipStream_t const next = hip_stream == DLMC_DEFAULT_STREAM ? nullptr
+                             : hip_stream                       ? (hipStream_t)hip_stream
+                                                                : m->own_stream;
+    // no wait in a capture, which it would end: a call that uses the model's buffers
+    // has waited for its work itself
+    if (!capturing(next) && !capturing(m->stream)) DLMC_HIP(hipStreamSynchronize(m->stream));
+    m->stream = next;
   });
 }
 

@@ -420,6 +420,43 @@ def test_streams_and_a_captured_graph():
             assert all(torch.equal(a, b) for a, b in zip(eager, want[(k + 1) % 3]))
 
 
+def test_a_capture_on_streams_the_model_has_not_seen():
+    """Eager calls on the default stream first; then a capture on one stream, with a
+    branch on another."""
+    V, K, n = 3001, 512, 9
+    g = torch.Generator().manual_seed(14)
+    with dl.Model(shape(vocab=V, n_layers=0), max_chunk=1) as m:
+        w = m.mx_quantize(torch.randn(V, K, generator=g).cuda(), "fp4")
+        x, y = torch.randn(n, K, generator=g).cuda(), torch.randn(n, K, generator=g).cuda()
+        tok = torch.zeros(n, dtype=torch.int32).cuda()
+        want = [t.clone() for t in chain(m, x, y.bfloat16(), w, tok)]
+        other = m.mx_matmul(m.mx_quantize(y, "fp8"), w)
+        torch.cuda.synchronize()
+        a, b = torch.cuda.Stream(), torch.cuda.Stream()
+        d = y.bfloat16()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        log("capture on new streams")
+        with torch.cuda.graph(graph, stream=a):
+            q = m.mx_quantize(y, "fp8")
+            b.wait_stream(a)
+            with torch.cuda.stream(b):
+                branch = m.mx_matmul(q, w)
+            out = chain(m, x, d, w, tok)
+            a.wait_stream(b)
+        for _ in range(3):
+            branch.zero_()
+            for t in out:
+                t.zero_()
+            torch.cuda.synchronize()
+            with torch.cuda.stream(a):
+                graph.replay()
+            a.synchronize()
+            assert all(torch.equal(s, t) for s, t in zip(out, want)) and torch.equal(branch, other)
+            eager = chain(m, x, d, w, tok)
+            assert all(torch.equal(s, t) for s, t in zip(eager, want))
+
+
 # ---------------------------------------------------------------- refusals
 def test_refusals(m):
     x = torch.randn(4, 64, device="cuda")
