@@ -337,7 +337,7 @@ mx_ring_kernel(MxArgs p) {
 
 // ---------------------------------------------------------------------------
 // 256 x 256 tiles by four waves, one per SIMD, each on 128 x 128 (256 accumulator
-// registers).  A wave reads eight fragments for sixteen instructions, and a tile
+// registers); with TM = 2 128 x 256, each wave on 64 x 128, BLOCKS of them a CU.  A wave reads eight fragments for sixteen instructions, and a tile
 // fills LDS with 68 KB (E2M1) or 100 KB (E4M3) per 256 columns, half as much per
 // product as 128-wide tiles: filling and reading LDS is what bounds these kernels.
 //
@@ -364,8 +364,8 @@ constexpr int wide_younger(int NS, int NL, int R, int st) {
   return n;
 }
 
-template <int FA, int TM, int NS, bool OUT_BF16>
-__global__ void __launch_bounds__(256, TM == 2 ? 2 : 1)
+template <int FA, int TM, int NS, int BLOCKS, bool OUT_BF16>
+__global__ void __launch_bounds__(256, BLOCKS)
 mx_wide_kernel(MxArgs p) {
   constexpr int WM = 32 * TM, BM = 2 * WM;
   constexpr int AROW = FA == DLMC_MX_FP4 ? 64 : 128, BROW = 64;  // bytes of a row in a stage
@@ -373,7 +373,7 @@ mx_wide_kernel(MxArgs p) {
   constexpr int A_IN = A_B / 4096, B_IN = B_B / 4096, NL = A_IN + B_IN, H1 = NS == 2 ? NL : NL / 2;
   constexpr int PF = 256 + 8;  // pitch of the staged output, in its elements
   constexpr int LDS = NS * STAGE + 2 * SC, OUT = OUT_BF16 ? BM * PF * 2 : 0;
-  static_assert(LDS <= (TM == 2 ? 80 : 160) * 1024 && OUT <= (TM == 2 ? 80 : 160) * 1024, "LDS");
+  static_assert(LDS <= 160 * 1024 / BLOCKS && OUT <= 160 * 1024 / BLOCKS && NS <= 4, "LDS / peeled groups");
   __shared__ __attribute__((aligned(16))) uint8_t smem[LDS > OUT ? LDS : OUT];
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -602,7 +602,7 @@ mx_wide_kernel(MxArgs p) {
   }
 }
 
-template <int FA, int TM, int NS>
+template <int FA, int TM, int NS, int BLOCKS>
 void launch_wide(hipStream_t st, MxArgs p, bool out_bf16) {
   p.n_tm = ceil_div(p.M, 64 * TM);
   p.n_tn = ceil_div(p.N, 256);
@@ -610,9 +610,9 @@ void launch_wide(hipStream_t st, MxArgs p, bool out_bf16) {
   DLMC_CHECK(tiles < (1ll << 24) - 8, DLMC_E_INVAL, "product with too many tiles");  // threads in 32 bits
   const unsigned grid = (unsigned)((tiles + 7) & ~7ll);
   if (out_bf16)
-    mx_wide_kernel<FA, TM, NS, true><<<grid, 256, 0, st>>>(p);
+    mx_wide_kernel<FA, TM, NS, BLOCKS, true><<<grid, 256, 0, st>>>(p);
   else
-    mx_wide_kernel<FA, TM, NS, false><<<grid, 256, 0, st>>>(p);
+    mx_wide_kernel<FA, TM, NS, BLOCKS, false><<<grid, 256, 0, st>>>(p);
   DLMC_HIP(hipGetLastError());
 }
 
@@ -632,10 +632,12 @@ void launch_ring(hipStream_t st, MxArgs p, bool out_bf16) {
 
 // Which kernel a product takes: the least of the times that these costs give.  us of
 // a tile beside its groups (start, epilogue), of a group of 256 columns where a CU has
-// one tile, and of a group per tile where it has many (`busy`: the tiles of a CU
-// share the filling and reading of its LDS).  Measured at 1 .. 8192 rows, 768 .. 12288
-// columns and widths of 2304 .. 126464, launches of one kernel each; a choice that is
-// off costs up to a fifth.  Some of what they come from, in us (E2M1 / E4M3):
+// one tile, and of a group per tile where it has more (`busy`: the tiles of a CU
+// share the filling and reading of its LDS); the CU with the most tiles counts.
+// Measured at 1 .. 8192 rows, 768 .. 12288 columns and widths of 2304 .. 126464,
+// launches of one kernel each; over a hundred sizes the choice takes 2.5% longer than
+// the fastest kernel on average, a fifth at most.  Some of what they come from, in us
+// (E2M1 / E4M3):
 //   rows x width x columns    32x64       32x128      64x64       64x128      128x256     256x256
 //       1 x   4096 x  4096    6.1 / 6.8   8.5 / 9.9   7.2 / 8.4    10 / 11     16 / 23     25 / 37
 //      16 x 126464 x  4096     40 / 44     40 / 40     43 / 54     47 / 44     46 / 61     64 / 93
@@ -645,17 +647,21 @@ void launch_ring(hipStream_t st, MxArgs p, bool out_bf16) {
 //    2048 x   4096 x  4096     48 / 70     40 / 46     32 / 42     30 / 36     22 / 37     31 / 42
 //    2048 x  12288 x  4096                             84 / 114    78 / 102    56 / 80     66 / 87
 // (2048 x 24576 x 4096 in E2M1: 128x256 128, 256x256 112.)
-enum TileKind { RING_32x64, RING_32x128, RING_64x64, RING_64x128, WIDE_128, WIDE_256, TILE_KINDS };
-constexpr int TILE_ROWS[TILE_KINDS] = {32, 32, 64, 64, 128, 256};
-constexpr int TILE_COLS[TILE_KINDS] = {64, 128, 64, 128, 256, 256};
+// WIDE_128_DEEP has the 128x256 tile's four stages in the LDS of a whole CU, for
+// launches of about a tile a CU: in E4M3 2048 x 4096 x 4096 39 -> 33 us, x 12288 105 ->
+// 83, 512 x 12288 x 4096 36 -> 27 (inputs from HBM); in E2M1, whose two blocks a CU
+// have three stages each, 25 us either way.
+enum TileKind { RING_32x64, RING_32x128, RING_64x64, RING_64x128, WIDE_128, WIDE_256, WIDE_128_DEEP, TILE_KINDS };
+constexpr int TILE_ROWS[TILE_KINDS] = {32, 32, 64, 64, 128, 256, 128};
+constexpr int TILE_COLS[TILE_KINDS] = {64, 128, 64, 128, 256, 256, 256};
 struct TileCost {
   float fixed, group, busy;
 };
 constexpr TileCost TILE_COST[2][TILE_KINDS] = {
     {{0.3f, 0.18f, 0.235f}, {0.3f, 0.375f, 0.42f}, {0.3f, 0.287f, 0.22f}, {0.8f, 0.45f, 0.41f}, {1.9f, 0.73f, 1.16f},
-     {9.7f, 1.15f, 1.55f}},
+     {9.7f, 1.15f, 1.55f}, {}},
     {{0.3f, 0.215f, 0.335f}, {0.4f, 0.47f, 0.465f}, {0.43f, 0.374f, 0.297f}, {1.1f, 0.55f, 0.533f}, {2.6f, 1.7f, 1.667f},
-     {12.0f, 1.94f, 2.05f}}};
+     {12.0f, 1.94f, 2.05f}, {4.0f, 1.4f, 1.4f}}};
 
 }  // namespace
 
@@ -683,9 +689,9 @@ void mx_matmul(hipStream_t st, MxView A, int fmt_a, size_t a_slots, MxView B, in
     const TileCost& c = TILE_COST[fmt_a == DLMC_MX_FP4 ? 0 : 1][k];
     // the wide kernels' offsets within a tile are 32 bits wide
     if (k >= WIDE_128 && p.groups >= 1 << 13) continue;
-    const float tiles = (float)ceil_div(rows, TILE_ROWS[k]) * (float)ceil_div(N, TILE_COLS[k]) / 256.0f;
-    const float each = k == WIDE_256 ? std::ceil(tiles) : tiles;  // alone on its CU: whole waves
-    const float us = c.fixed * std::max(each, 1.0f) + (float)p.groups * std::max(c.group, each * c.busy);
+    const float each = std::ceil((float)ceil_div(rows, TILE_ROWS[k]) * (float)ceil_div(N, TILE_COLS[k]) / 256.0f);
+    if (k == WIDE_128_DEEP && fmt_a == DLMC_MX_FP4) continue;  // no faster than with three stages
+    const float us = c.fixed * each + (float)p.groups * std::max(c.group, each * c.busy);
     if (k == 0 || us < least) {
       best = k;
       least = us;
@@ -697,8 +703,8 @@ void mx_matmul(hipStream_t st, MxView A, int fmt_a, size_t a_slots, MxView B, in
       case RING_32x128: return launch_ring<DLMC_MX_FP4, 32, 128, 1, 4, 3, false>(st, p, out_bf16);
       case RING_64x64: return launch_ring<DLMC_MX_FP4, 64, 64, 2, 2, 2, false>(st, p, out_bf16);
       case RING_64x128: return launch_ring<DLMC_MX_FP4, 64, 128, 2, 2, 2, false>(st, p, out_bf16);
-      case WIDE_128: return launch_wide<DLMC_MX_FP4, 2, 3>(st, p, out_bf16);
-      default: return launch_wide<DLMC_MX_FP4, 4, 4>(st, p, out_bf16);
+      case WIDE_128: return launch_wide<DLMC_MX_FP4, 2, 3, 2>(st, p, out_bf16);
+      default: return launch_wide<DLMC_MX_FP4, 4, 4, 1>(st, p, out_bf16);
     }
   }
   switch (best) {
@@ -706,8 +712,9 @@ void mx_matmul(hipStream_t st, MxView A, int fmt_a, size_t a_slots, MxView B, in
     case RING_32x128: return launch_ring<DLMC_MX_FP8, 32, 128, 1, 4, 3, false>(st, p, out_bf16);
     case RING_64x64: return launch_ring<DLMC_MX_FP8, 64, 64, 2, 2, 2, false>(st, p, out_bf16);
     case RING_64x128: return launch_ring<DLMC_MX_FP8, 64, 128, 2, 2, 2, false>(st, p, out_bf16);
-    case WIDE_128: return launch_wide<DLMC_MX_FP8, 2, 2>(st, p, out_bf16);
-    default: return launch_wide<DLMC_MX_FP8, 4, 3>(st, p, out_bf16);
+    case WIDE_128: return launch_wide<DLMC_MX_FP8, 2, 2, 2>(st, p, out_bf16);
+    case WIDE_128_DEEP: return launch_wide<DLMC_MX_FP8, 2, 4, 1>(st, p, out_bf16);
+    default: return launch_wide<DLMC_MX_FP8, 4, 3, 1>(st, p, out_bf16);
   }
 }
 
