@@ -543,27 +543,34 @@ scores_join_kernel(ScoreArgs p) {
   write_row(p, row, merge_lanes(s), key, id, n, lane, tok, tok_logit);
 }
 
-// Whether each wave takes a row: where a row is a tile or two, or there are rows for
-// half of the chip's waves; with 512 rows up to ten tiles, which take a wave no longer
-// than a block's waves take to join.  us with 0 / 5 / 20 alternatives, a row a block and
-// a row a wave, fp32:
+// Whether each wave takes a row: where a row is a tile or two, or the blocks would not
+// all be on the chip at once (256 CUs hold eight each).  Then the joining of a block's
+// waves costs most, unless rows are so long that a CU's 32 rows at a time keep less of
+// memory busy than eight: without alternatives, whose joining is short, from ten tiles
+// on, and with alternatives up to 4096 rows from twenty on.  us with 0 / 8 / 20
+// alternatives, a row a block and a row a wave, fp32 (bf16 where marked):
+//    3000 x  1000   8.5 /  18 /  23    6.8 /  11 /  14
+//    1272 x  2000   5.3 /  12 /  13    6.1 /  13 /  15
+//    1272 x  4099   7.8 /  15 /  16    9.2 /  21 /  23
+//    2500 x  4099    12 /  25 /  28     11 /  24 /  25
+//    3000 x  9000    24 /  46 /  50     24 /  42 /  41
+//    5000 x 20000    82 / 112 / 123     82 /  98 /  96
+//    5000 x 20000    47 /  87 / 107     53 /  79 /  84  bf16
 //   42115 x   265    52 / 146 / 223     18 /  39 /  55
 //   44113 x  4099   144 / 279 / 368    125 / 172 / 220
-//    4096 x 32768   108 / 128 / 146    105 / 125 / 128
-//    1000 x  4099    11 /  22 /  27    8.7 /  19 /  21
-//     100 x  4099   6.1 /  13 /  15    6.4 /  16 /  19
-//    2000 x  8000    16 /  28 /  34     21 /  35 /  36
-//    1000 x 32768    31 /  49 /  58     54 /  81 /  87
-bool rows_by_waves(int n_rows, int V) {
-  return V <= 2 * TILE || n_rows >= 4096 || (n_rows >= 512 && V <= 10 * TILE);
+//    2100 x126464   237 / 277 / 259    267 / 311 / 324
+bool rows_by_waves(int n_rows, int V, int n_top) {
+  if (V <= 2 * TILE) return true;
+  if (n_rows <= 2048) return false;
+  return n_top ? n_rows >= 4096 || V <= 20 * TILE : V <= 10 * TILE;
 }
 
 // Blocks a row's columns are split over: enough blocks for the chip's 256 CUs eight
 // times over, but at least two tiles to a wave, and three blocks, as joining costs a
 // launch (1000 x 32768 with 5 alternatives in two 49 us, unsplit 45; 600 x 126464 in
 // three 86, unsplit 113).
-int splits_of(int n_rows, int V) {
-  if (rows_by_waves(n_rows, V)) return 1;
+int splits_of(int n_rows, int V, int n_top) {
+  if (rows_by_waves(n_rows, V, n_top)) return 1;
   const int s = std::min({2048 / n_rows, ceil_div(V + 7, 8 * TILE), MAX_SPLIT});
   return s < 3 ? 1 : s;
 }
@@ -571,7 +578,7 @@ int splits_of(int n_rows, int V) {
 }  // namespace
 
 size_t token_scores_ws(int n_rows, int V, int n_top) {
-  const int s = n_rows > 0 ? splits_of(n_rows, V) : 1;
+  const int s = n_rows > 0 ? splits_of(n_rows, V, n_top) : 1;
   return s == 1 ? 0 : (size_t)n_rows * s * record_bytes(n_top);
 }
 
@@ -588,8 +595,8 @@ void token_scores(hipStream_t st, const void* logits, bool bf16, size_t ld, int 
                    n_top ? top_logp + r * n_top : nullptr, ws);
     return;
   }
-  ScoreArgs p{logits, ld, n_rows, V, splits_of(n_rows, V), n_top, tokens, logp, entropy, top_ids, top_logp, (uint8_t*)ws};
-  const bool wave_rows = rows_by_waves(n_rows, V);
+  ScoreArgs p{logits, ld, n_rows, V, splits_of(n_rows, V, n_top), n_top, tokens, logp, entropy, top_ids, top_logp, (uint8_t*)ws};
+  const bool wave_rows = rows_by_waves(n_rows, V, n_top);
   const unsigned grid = wave_rows ? (unsigned)ceil_div(n_rows, 4) : (unsigned)n_rows * p.splits;
   auto go = [&](auto four, auto one) { (wave_rows ? four : one)<<<grid, 256, 0, st>>>(p); };
   if (n_top == 0)

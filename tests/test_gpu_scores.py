@@ -72,8 +72,8 @@ def test_many_rows(n, V):
         check(got, reference(lg, tok, 5), V)
 
 
-@pytest.mark.parametrize("n,V", [(3, 1023), (3, 1024), (3, 1025), (511, 5120), (512, 5120), (513, 5121), (682, 9000),
-                                 (683, 9000), (4095, 6000), (4096, 6000), (4099, 6000)])
+@pytest.mark.parametrize("n,V", [(3, 1023), (3, 1024), (3, 1025), (511, 5120), (682, 9000), (683, 9000), (2048, 5120),
+                                 (2049, 5120), (2049, 5121), (2051, 10240), (2051, 10241), (4095, 11000), (4097, 11000)])
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 def test_either_side_of_the_launchs_choices(n, V, dtype):
     """A row to a wave, to a block, or to several blocks; rows that do not fill a block."""
