@@ -661,7 +661,7 @@ constexpr TileCost TILE_COST[2][TILE_KINDS] = {
     {{0.3f, 0.18f, 0.235f}, {0.3f, 0.375f, 0.42f}, {0.3f, 0.287f, 0.22f}, {0.8f, 0.45f, 0.41f}, {1.9f, 0.73f, 1.16f},
      {9.7f, 1.15f, 1.55f}, {}},
     {{0.3f, 0.215f, 0.335f}, {0.4f, 0.47f, 0.465f}, {0.43f, 0.374f, 0.297f}, {1.1f, 0.55f, 0.533f}, {2.6f, 1.7f, 1.667f},
-     {12.0f, 1.94f, 2.05f}, {4.0f, 1.4f, 1.4f}}};
+     {12.0f, 1.94f, 2.05f}, {3.5f, 1.4f, 1.4f}}};
 
 }  // namespace
 

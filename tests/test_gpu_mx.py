@@ -254,6 +254,35 @@ def test_product_of_many_tiles(m, fmt, M, N, K):
     check_product(m, qa, qb, m.mx_matmul(qa, qb), fmt)
 
 
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+@pytest.mark.parametrize("M,N,K", [(2048, 4096, 1000), (1900, 4090, 1281), (300, 17001, 2000), (129, 32768, 1537)])
+def test_product_of_about_a_tile_a_cu(m, fmt, M, N, K):
+    """And the same bits for its last rows in a launch of their own."""
+    log("product", fmt, M, N, K)
+    qa, qb = operands(m, M, N, K, fmt)
+    out = m.mx_matmul(qa, qb)
+    check_product(m, qa, qb, out, fmt)
+    assert torch.equal(m.mx_matmul(rows_of(qa, M - 33, M), qb), out[M - 33:])
+    assert torch.equal(m.mx_matmul(qa, qb, torch.bfloat16), out.bfloat16())
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+def test_product_over_many_columns(m, fmt):
+    """Groups past those that the wide tiles' 32-bit offsets take (2^21 columns)."""
+    M, N, K = 40, 70, 2200001
+    log("columns", fmt, K)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    # integers that E2M1 holds: their products and sums up to 2^24 are exact in fp32
+    a = torch.randint(0, 3, (M, K), generator=g, device="cuda", dtype=torch.int32).float()
+    b = torch.randint(-1, 2, (N, K), generator=g, device="cuda", dtype=torch.int32).float()
+    a[:, ::32], b[:, ::32] = 6, -6  # a block's scale is 1, or 2^-6 with E4M3's 448 above 6 2^6
+    qa, qb = m.mx_quantize(a, fmt), m.mx_quantize(b, "fp4")
+    a, b = a.double(), b.double()
+    assert torch.equal(m.mx_dequantize(qa, torch.float32).double(), a)
+    assert torch.equal(m.mx_dequantize(qb, torch.float32).double(), b)
+    assert torch.equal(m.mx_matmul(qa, qb).double(), a @ b.t())
+
+
 def rows_of(q, lo, hi):
     """Rows lo .. hi - 1 of q, their codes and scales as they are.  (Quantising the
     values again may hold them with another scale: the same values in other codes,
