@@ -341,6 +341,7 @@ class Model:
         self.handle = h
         self.device = device
         self._trace_cb = None
+        self._ws_sizes = {}
         self._stream = None  # what set_stream was last given
         self._hook_stream = False  # whether that was a stage hook's default stream
 
@@ -709,6 +710,17 @@ class Model:
         self._call(lib().dlmc_mx_matmul, ac, asc, MX_FORMAT[a.fmt], bc, bsc, M, N, K, optr, code, ldo)
         return out
 
+    def _scores_ws(self, n: int, top: int) -> int:
+        """Bytes of workspace, which go by the sizes alone (asked for once each)."""
+        need = self._ws_sizes.get((n, top))
+        if need is None:
+            size = u64(0)
+            _check(lib().dlmc_token_scores_ws(self.handle, n, top, ctypes.byref(size)))
+            if len(self._ws_sizes) >= 64:
+                self._ws_sizes.clear()
+            need = self._ws_sizes[n, top] = size.value
+        return need
+
     def token_scores(self, logits, tokens=None, top: int = 0):
         """Of logits [n, vocab] (fp32 or bf16): (log2 probability of tokens[i] in row
         i (None without tokens), entropy in bits, ids [n, top] of the most probable
@@ -728,12 +740,9 @@ class Model:
         H = logits.new_empty(n, dtype=f32t)
         ids = logits.new_empty((n, top), dtype=i32t)
         tlp = logits.new_empty((n, top), dtype=f32t)
-        need = u64(0)
-        L = lib()
-        _check(L.dlmc_token_scores_ws(self.handle, n, top, ctypes.byref(need)))
-        need = need.value
+        need = self._scores_ws(n, top)
         ws = logits.new_empty(need, dtype=torch.uint8) if need else None
-        self._call(L.dlmc_token_scores, ptr, code, ld, n, tptr, top, lptr, H.data_ptr(), ids.data_ptr(),
+        self._call(lib().dlmc_token_scores, ptr, code, ld, n, tptr, top, lptr, H.data_ptr(), ids.data_ptr(),
                    tlp.data_ptr(), ws.data_ptr() if need else None, need)
         return logp, H, ids, tlp
 

@@ -454,11 +454,18 @@ scores_kernel(ScoreArgs p) {
   s = merge(merge(stats[0], stats[1]), merge(stats[2], stats[3]));
   uint32_t key = 0, id = 0xFFFFFFFFu;
   if constexpr (TOP) {
-    constexpr int E = 4 * ((CUT + 63) / 64);
-    uint32_t ke[E], ie[E], bound;
+    auto join = [&](auto each_) {
+      constexpr int EACH = decltype(each_)::value, E = 4 * EACH;
+      uint32_t ke[E], ie[E], bound;
 #pragma unroll
-    for (int e = 0; e < E; ++e) entry(e & 3, e >> 2, counts[e & 3], ke[e], ie[e]);
-    n = narrow<E>(ke, ie, p.k, 64, wk, wi, bound);
+      for (int e = 0; e < E; ++e) entry(e & 3, e >> 2, counts[e & 3], ke[e], ie[e]);
+      n = narrow<E>(ke, ie, p.k, 64, wk, wi, bound);
+    };
+    // mostly the lists have an entry a lane at most
+    if (max(max(counts[0], counts[1]), max(counts[2], counts[3])) <= 64)
+      join(std::integral_constant<int, 1>{});
+    else
+      join(std::integral_constant<int, (CUT + 63) / 64>{});
     if (lane < n) {
       key = wk[lane];
       id = wi[lane];
