@@ -183,7 +183,12 @@ __device__ __forceinline__ uint32_t bound_of(const uint32_t (&key)[E], int k) {
 
 // The entries that may be among the k best, side by side in keys / ids: at most
 // `most` of them, k where the bound leaves more.  Sets a bound that k of them reach.
-template <int E>
+// MOVE: keys and ids have room for NARROW_ROOM entries; what the bound leaves is moved
+// there and cut as four entries a lane instead of E (the cut counts every entry 32
+// times: one row with 64 alternatives 31 -> 25 us).  With few alternatives, whose bound
+// leaves few, the added code costs up to 8%.
+constexpr int NARROW_ROOM = 256;
+template <int E, bool MOVE>
 __device__ __forceinline__ int narrow(const uint32_t (&key)[E], const uint32_t (&id)[E], int k, int most,
                                       uint32_t* keys, uint32_t* ids, uint32_t& bound) {
   bool keep[E];
@@ -193,6 +198,23 @@ __device__ __forceinline__ int narrow(const uint32_t (&key)[E], const uint32_t (
   for (int e = 0; e < E; ++e) {
     keep[e] = key[e] != 0 && key[e] >= bound;
     n += count(keep[e]);
+  }
+  if constexpr (MOVE) {
+    if (n > most && n <= NARROW_ROOM) {
+      pack<E>(key, id, keep, keys, ids);
+      constexpr int F = NARROW_ROOM / 64;
+      uint32_t ke[F], ie[F];
+      bool kept[F];
+      const int lane = __lane_id();
+#pragma unroll
+      for (int e = 0; e < F; ++e) {
+        const int at = e * 64 + lane;
+        ke[e] = at < n ? keys[at] : 0u;
+        ie[e] = at < n ? ids[at] : 0xFFFFFFFFu;
+      }
+      bound = cut<F>(ke, ie, k, kept);
+      return pack<F>(ke, ie, kept, keys, ids);
+    }
   }
   if (n > most) bound = cut<E>(key, id, k, keep);
   return pack<E>(key, id, keep, keys, ids);
@@ -282,6 +304,7 @@ __global__ void __launch_bounds__(256, CUT == LONG_LIST ? 6 : 8)
 scores_kernel(ScoreArgs p) {
   constexpr bool TOP = CUT > 0;
   constexpr int LIST = CUT + TILE;
+  static_assert(LIST >= NARROW_ROOM, "room of a wave's list");
   __shared__ uint32_t keys[TOP ? 4 : 1][TOP ? LIST : 1], ids[TOP ? 4 : 1][TOP ? LIST : 1];
   __shared__ Stat stats[4];
   __shared__ int counts[4];
@@ -341,7 +364,7 @@ scores_kernel(ScoreArgs p) {
     uint32_t key[E], id[E], bound;
 #pragma unroll
     for (int e = 0; e < E; ++e) entry(wave, e, n, key[e], id[e]);
-    n = narrow<E>(key, id, p.k, CUT, wk, wi, bound);
+    n = narrow<E, CUT == LONG_LIST>(key, id, p.k, CUT, wk, wi, bound);
     thr = value_of(max(bound, LEAST_KEY));
   };
 
@@ -437,7 +460,7 @@ scores_kernel(ScoreArgs p) {
       uint32_t ke[E], ie[E], bound;
 #pragma unroll
       for (int e = 0; e < E; ++e) entry(wave, e, n, ke[e], ie[e]);
-      if (n > 64) n = narrow<E>(ke, ie, p.k, 64, wk, wi, bound);
+      if (n > 64) n = narrow<E, (E > 4 && CUT == LONG_LIST)>(ke, ie, p.k, 64, wk, wi, bound);
       if (lane < n) {
         key = wk[lane];
         id = wi[lane];
@@ -459,7 +482,7 @@ scores_kernel(ScoreArgs p) {
       uint32_t ke[E], ie[E], bound;
 #pragma unroll
       for (int e = 0; e < E; ++e) entry(e & 3, e >> 2, counts[e & 3], ke[e], ie[e]);
-      n = narrow<E>(ke, ie, p.k, 64, wk, wi, bound);
+      n = narrow<E, (E > 4 && CUT == LONG_LIST)>(ke, ie, p.k, 64, wk, wi, bound);
     };
     // mostly the lists have an entry a lane at most
     if (max(max(counts[0], counts[1]), max(counts[2], counts[3])) <= 64)
@@ -492,7 +515,7 @@ template <bool BF16>
 __global__ void __launch_bounds__(256)
 scores_join_kernel(ScoreArgs p) {
   constexpr int EACH = MAX_SPLIT / 4;
-  __shared__ uint32_t keys[4][MAX_TOP], ids[4][MAX_TOP];
+  __shared__ uint32_t keys[4][NARROW_ROOM], ids[4][NARROW_ROOM];
   __shared__ int counts[4];
   const int row = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const size_t rec = record_bytes(p.k);
@@ -528,7 +551,7 @@ scores_join_kernel(ScoreArgs p) {
         ++from;
       }
     }
-    n = total > 0 ? narrow<EACH>(ke, ie, p.k, MAX_TOP, keys[wave], ids[wave], bound) : 0;
+    n = total > 0 ? narrow<EACH, true>(ke, ie, p.k, MAX_TOP, keys[wave], ids[wave], bound) : 0;
     if (!alone) {
       if (lane == 0) counts[wave] = n;
       __syncthreads();
@@ -540,7 +563,7 @@ scores_join_kernel(ScoreArgs p) {
         k4[e] = in ? keys[e][lane] : 0u;
         i4[e] = in ? ids[e][lane] : 0xFFFFFFFFu;
       }
-      n = narrow<4>(k4, i4, p.k, MAX_TOP, keys[0], ids[0], bound);
+      n = narrow<4, false>(k4, i4, p.k, MAX_TOP, keys[0], ids[0], bound);
     }
     if (lane < n) {
       key = keys[0][lane];
