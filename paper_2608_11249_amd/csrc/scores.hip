@@ -23,10 +23,11 @@ namespace dlmc {
 namespace {
 
 constexpr int TILE = 512;            // columns a wave takes at a time, eight a lane
-// Entries of a wave's list before it is cut (a whole tile fits on top): with 96 a CU
-// holds eight blocks, so that 2048 rows are on the chip at once; with more
-// alternatives than 16 it would be cut too often.
-constexpr int FEW_TOP = 16, FEW_LIST = 96, LONG_LIST = 256;
+// Entries of a wave's list before it is cut: with 96, and room for a tile on top, a CU
+// holds eight blocks, so that 2048 rows are on the chip at once.  With more
+// alternatives than 16 it would be cut too often: 192, and room for half a tile (2048 x
+// 126464 with 20 alternatives 208 us; with 256 and a whole tile, six blocks a CU, 255).
+constexpr int FEW_TOP = 16, FEW_LIST = 96, LONG_LIST = 192;
 constexpr int MAX_SPLIT = 32, MAX_TOP = 64;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float NEG_INF = -__builtin_inff();
@@ -300,10 +301,10 @@ __device__ __forceinline__ Stat merge_lanes(Stat s) {
 // ROWS 1: a row, or one of its `splits` parts, by a block's four waves; ROWS 4: a row
 // by each of them.  CUT: entries before a list is cut, 0 without alternatives.
 template <bool BF16, int CUT, int ROWS>
-__global__ void __launch_bounds__(256, CUT == LONG_LIST ? 6 : 8)
+__global__ void __launch_bounds__(256, 8)
 scores_kernel(ScoreArgs p) {
   constexpr bool TOP = CUT > 0;
-  constexpr int LIST = CUT + TILE;
+  constexpr int ROOM = CUT == LONG_LIST ? TILE / 2 : TILE, LIST = CUT + ROOM;
   static_assert(LIST >= NARROW_ROOM, "room of a wave's list");
   __shared__ uint32_t keys[TOP ? 4 : 1][TOP ? LIST : 1], ids[TOP ? 4 : 1][TOP ? LIST : 1];
   __shared__ Stat stats[4];
@@ -410,30 +411,37 @@ scores_kernel(ScoreArgs p) {
           ties = true;
         }
       }
-      auto push = [&](bool in, int i) {
+      auto push = [&](bool in, float x, int c) {
         const uint64_t mask = __ballot(in);
         if (mask == 0) return;
         if (in) {
           const int at = n + rank_in(mask);
-          wk[at] = order_of(v[i]);
-          wi[at] = (uint32_t)(column(t, i / CH) + i % CH);
+          wk[at] = order_of(x);
+          wi[at] = (uint32_t)c;
         }
         n += __popcll(mask);
       };
       const bool all = ties && thr == NEG_INF;  // -inf too, but nothing beside the row
       // where ties count, what lies above the number before the threshold
-      const float above = ties ? before(thr) : thr;
+      float above = ties ? before(thr) : thr;
       if (all || __any(top > above)) {
+        constexpr int PARTS = TILE / ROOM, EACH = 8 / PARTS;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          bool in = v[i] > above;
-          if (all) {
-            const int c = column(t, i / CH) + i % CH;
-            in = v[i] >= thr && c >= 0 && c < p.V;
+        for (int h = 0; h < PARTS; ++h) {
+#pragma unroll
+          for (int j = 0; j < EACH; ++j) {
+            const float x = PARTS == 1 || h == 0 ? v[j] : v[8 - EACH + j];
+            const int c = PARTS == 1 ? column(t, j / CH) + j % CH : CH == 8 ? column(t, 0) + h * EACH + j : column(t, h) + j;
+            bool in = x > above;
+            if (all) in = x >= thr && c >= 0 && c < p.V;
+            push(in, x, c);
           }
-          push(in, i);
+          if (n > CUT) {
+            shrink();
+            // the tile's other part may have lower ids
+            if (PARTS > 1 && thr > NEG_INF) above = before(thr);
+          }
         }
-        if (n > CUT) shrink();
       }
     }
   };

@@ -113,6 +113,29 @@ def test_ties_and_orders(V):
             assert np.array_equal(got[2].cpu().numpy(), np.tile(want[2], (250, 1)))
 
 
+@pytest.mark.parametrize("V", [600, 1500, 5000, 40001])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_ties_where_lists_fill_up(V, dtype):
+    """Rows that rise, so that every tile lies above what came before, in steps of equal
+    logits, of a lane's eight in either order, and of -inf: the lists are cut in the
+    middle of a tile, whose later columns hold equal logits of lower and higher ids."""
+    r = np.random.default_rng(V)
+    at = np.arange(V)
+    lg = np.stack([at // 37, at // 8 % 64, at % 8, 7 - at % 8, at // 4 % 2 + at // 512, r.integers(0, 2, V),
+                   at // 300, np.where(at % 5, -np.inf, at // 100), np.where(at < V - 20, -np.inf, 1.0),
+                   np.where(at // 256 % 2, at // 512, -at // 512), -(at // 90), np.zeros(V)])
+    lg = torch.from_numpy(lg.astype(np.float32)).to(getattr(torch, dtype)).cuda()
+    for many in (1, 260):
+        x = lg.repeat(many, 1)
+        if many > 1 and V == 40001:
+            x = x[:2500]
+        want = torch.sort(x, dim=1, descending=True, stable=True)[1]
+        with model(V) as m:
+            for top in (3, 16, 17, 40, 64):
+                log("lists", V, dtype, many, top)
+                assert torch.equal(m.token_scores(x, top=top)[2], want[:, :top].int()), top
+
+
 @pytest.mark.parametrize("V", [100, 3000, 126464])
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 def test_masked_symbols(V, dtype):
