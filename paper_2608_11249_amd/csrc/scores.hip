@@ -587,16 +587,16 @@ scores_join_kernel(ScoreArgs p) {
 // memory busy than eight: without alternatives, whose joining is short, from ten tiles
 // on, and with alternatives up to 4096 rows from twenty on.  us with 0 / 8 / 20
 // alternatives, a row a block and a row a wave, fp32 (bf16 where marked):
-//    3000 x  1000   8.5 /  18 /  23    6.8 /  11 /  14
-//    1272 x  2000   5.3 /  12 /  13    6.1 /  13 /  15
-//    1272 x  4099   7.8 /  15 /  16    9.2 /  21 /  23
-//    2500 x  4099    12 /  25 /  28     11 /  24 /  25
-//    3000 x  9000    24 /  46 /  50     24 /  42 /  41
-//    5000 x 20000    82 / 112 / 123     82 /  98 /  96
-//    5000 x 20000    47 /  87 / 107     53 /  79 /  84  bf16
-//   42115 x   265    52 / 146 / 223     18 /  39 /  55
-//   44113 x  4099   144 / 279 / 368    125 / 172 / 220
-//    2100 x126464   237 / 277 / 259    267 / 311 / 324
+//    3000 x  1000   6.7 /  16 /  17    5.8 /  10 /  12
+//    1272 x  2000   5.4 /  11 /  12    6.1 /  13 /  15
+//    1272 x  4099   7.9 /  15 /  16    9.2 /  21 /  23
+//    2500 x  4099    12 /  23 /  25     11 /  23 /  26
+//    3000 x  9000    24 /  42 /  46     24 /  40 /  43
+//    5000 x 20000    78 / 105 / 112     77 /  92 /  98
+//    5000 x 20000    47 /  89 /  97     52 /  80 /  87  bf16
+//   42115 x   265    52 / 140 / 129     18 /  38 /  46
+//   44113 x  4099   141 / 262 / 265    125 / 170 / 192
+//    2100 x126464   241 / 272 / 285    250 / 306 / 323
 bool rows_by_waves(int n_rows, int V, int n_top) {
   if (V <= 2 * TILE) return true;
   if (n_rows <= 2048) return false;
