@@ -77,18 +77,22 @@ __device__ __forceinline__ void put8(uint8_t* codes, size_t pitch, uint8_t* scal
 }
 
 // Groups of columns that a block of mx_quantize / mx_dequantize takes of each of
-// its eight rows (32 lanes to a group, eight columns a lane).
-constexpr int Q_GROUPS = 4;
+// its eight rows (32 lanes to a group, eight columns a lane).  HBM bound: 32768 x 4096
+// from bf16 to E2M1 61 us, 5.6 TB/s, and back to bf16 59 us.  The blocks of a row follow
+// each other, so that what is in flight lies together in memory (rows first: 73 and
+// 73); four groups a block take 64 and 59.
+constexpr int Q_GROUPS = 2;
 
 template <int FMT, bool BF16, bool VEC>
 __global__ void __launch_bounds__(256)
 mx_quantize_kernel(const void* __restrict__ x, size_t ldx, int rows, int cols, uint8_t* __restrict__ codes,
                    size_t pitch, uint8_t* __restrict__ scales, size_t slots, int groups) {
-  const int row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const int parts = (groups + Q_GROUPS - 1) / Q_GROUPS;
+  const int row = blockIdx.x / parts * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (row >= rows) return;  // whole halves of a wave
   const void* xr = (const uint8_t*)x + (size_t)row * ldx * (BF16 ? 2 : 4);
   float v[Q_GROUPS][8];
-  const int g0 = blockIdx.y * Q_GROUPS;
+  const int g0 = blockIdx.x % parts * Q_GROUPS;
 #pragma unroll
   for (int e = 0; e < Q_GROUPS; ++e) load8<BF16, VEC>(xr, (g0 + e) * MX_GROUP + lane * 8, cols, v[e]);
 #pragma unroll
@@ -100,10 +104,11 @@ template <int FMT, bool BF16, bool VEC>
 __global__ void __launch_bounds__(256)
 mx_dequantize_kernel(const uint8_t* __restrict__ codes, size_t pitch, const uint8_t* __restrict__ scales,
                      size_t slots, int rows, int cols, int groups, void* __restrict__ out, size_t ldo) {
-  const int row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const int parts = (groups + Q_GROUPS - 1) / Q_GROUPS;
+  const int row = blockIdx.x / parts * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (row >= rows) return;
   void* orow = (uint8_t*)out + (size_t)row * ldo * (BF16 ? 2 : 4);
-  const int g0 = blockIdx.y * Q_GROUPS;
+  const int g0 = blockIdx.x % parts * Q_GROUPS;
   uint32_t lo[Q_GROUPS], hi[Q_GROUPS], s[Q_GROUPS];
 #pragma unroll
   for (int e = 0; e < Q_GROUPS; ++e) {
@@ -139,7 +144,8 @@ __device__ __forceinline__ float wave_total(float t) {
 // wave a row a block takes four rows.  Which form a row takes goes by its
 // columns alone, so its sums, and with them its codes, do not depend on the
 // number of rows.  HBM bound: x and delta are read once, and everything is in
-// flight before the first value is used.
+// flight before the first value is used (2048 x 4096 in fp32 with a bf16 delta, to E4M3:
+// 17.5 us, 5.3 TB/s).
 template <int FMT, bool XB, bool VEC, int WAVES, int PER>
 __global__ void __launch_bounds__(256)
 add_norm_mx_kernel(AddNormMx a) {
@@ -238,8 +244,8 @@ void launch_add_norm(hipStream_t st, const AddNormMx& a) {
     add_norm_mx_kernel<FMT, XB, VEC, 4, 4><<<a.rows, 256, 0, st>>>(a);
 }
 
-// Rows of a launch: a grid's threads are counted in 32 bits.
-constexpr int LAUNCH_ROWS = 1 << 23;
+// Blocks of a launch: a grid's threads are counted in 32 bits.
+constexpr int LAUNCH_BLOCKS = 1 << 23;
 
 inline bool whole16(const void* p, size_t ld, size_t esz) {
   return ((uintptr_t)p & 15) == 0 && ld * esz % 16 == 0;
@@ -253,9 +259,10 @@ void mx_quantize(hipStream_t st, const void* x, bool bf16, size_t ldx, int rows,
   const size_t esz = bf16 ? 2 : 4, pitch = mx_pitch(fmt, cols);
   const bool vec = cols % 8 == 0 && whole16(x, ldx, esz);
   auto go = [&](auto kernel) {
-    for (size_t r = 0; r < (size_t)rows; r += LAUNCH_ROWS) {
-      const int n = (int)std::min<size_t>(rows - r, LAUNCH_ROWS);
-      const dim3 grid((unsigned)ceil_div(n, 8), (unsigned)ceil_div(groups, Q_GROUPS));
+    const size_t parts = ceil_div(groups, Q_GROUPS), most = LAUNCH_BLOCKS / parts * 8;
+    for (size_t r = 0; r < (size_t)rows; r += most) {
+      const int n = (int)std::min<size_t>(rows - r, most);
+      const unsigned grid = (unsigned)(ceil_div(n, 8) * parts);
       kernel<<<grid, 256, 0, st>>>((const uint8_t*)x + r * ldx * esz, ldx, n, cols, q.codes + r * pitch, pitch,
                                    q.scales + r * 8, mx_slots(rows), groups);
     }
@@ -276,9 +283,10 @@ void mx_dequantize(hipStream_t st, MxView q, int fmt, int rows, int cols, void* 
   const size_t esz = bf16 ? 2 : 4, pitch = mx_pitch(fmt, cols);
   const bool vec = cols % 8 == 0 && whole16(out, ldo, esz);
   auto go = [&](auto kernel) {
-    for (size_t r = 0; r < (size_t)rows; r += LAUNCH_ROWS) {
-      const int n = (int)std::min<size_t>(rows - r, LAUNCH_ROWS);
-      const dim3 grid((unsigned)ceil_div(n, 8), (unsigned)ceil_div(groups, Q_GROUPS));
+    const size_t parts = ceil_div(groups, Q_GROUPS), most = LAUNCH_BLOCKS / parts * 8;
+    for (size_t r = 0; r < (size_t)rows; r += most) {
+      const int n = (int)std::min<size_t>(rows - r, most);
+      const unsigned grid = (unsigned)(ceil_div(n, 8) * parts);
       kernel<<<grid, 256, 0, st>>>(q.codes + r * pitch, pitch, q.scales + r * 8, mx_slots(rows), n, cols, groups,
                                    (uint8_t*)out + r * ldo * esz, ldo);
     }
@@ -298,13 +306,13 @@ void add_norm_mx(hipStream_t st, AddNormMx a) {
   DLMC_CHECK(a.cols >= 1 && a.cols <= ADD_NORM_MAX_COLS, DLMC_E_INVAL, "norm of more columns than a block holds");
   a.pitch_cols = mx_groups(a.cols) * MX_GROUP;
   a.pitch = mx_pitch(a.fmt, a.cols);
-  if (a.rows > LAUNCH_ROWS) {
+  if (a.rows > LAUNCH_BLOCKS) {
     DLMC_CHECK(!a.gather && !a.n_dev, DLMC_E_INVAL, "too many gathered rows");
     const AddNormMx all = a;
     const size_t xs = a.x_bf16 ? 2 : 4, ds = a.delta_bf16 ? 2 : 4;
-    for (size_t r = 0; r < (size_t)all.rows; r += LAUNCH_ROWS) {
+    for (size_t r = 0; r < (size_t)all.rows; r += LAUNCH_BLOCKS) {
       AddNormMx part = all;
-      part.rows = (int)std::min<size_t>(all.rows - r, LAUNCH_ROWS);
+      part.rows = (int)std::min<size_t>(all.rows - r, LAUNCH_BLOCKS);
       part.x = (const uint8_t*)all.x + r * all.ldx * xs;
       if (all.delta) part.delta = (const uint8_t*)all.delta + r * all.ldd * ds;
       if (all.sum) part.sum = (uint8_t*)all.sum + r * all.lds * xs;
