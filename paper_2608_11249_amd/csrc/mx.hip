@@ -7,23 +7,20 @@ namespace dlmc {
 namespace {
 
 // Columns col .. col + 7 of a row as fp32, zeros from column cols on.  VEC: cols
-// and the row are whole 16-byte chunks.
+// and the row are whole 16-byte chunks; otherwise the chunks are loaded all the same,
+// at their elements' alignment, and a row's last columns one by one.
 template <bool BF16, bool VEC>
 __device__ __forceinline__ void load8(const void* row, int col, int cols, float (&v)[8]) {
+  const uint8_t* p = (const uint8_t*)row + (size_t)col * (BF16 ? 2 : 4);
+  u32x4 a{}, b{};
   if constexpr (VEC) {
-    u32x4 a{}, b{};
     if (col < cols) {
-      const u32x4* p = reinterpret_cast<const u32x4*>((const uint8_t*)row + (size_t)col * (BF16 ? 2 : 4));
-      a = p[0];
-      if constexpr (!BF16) b = p[1];
+      a = *reinterpret_cast<const u32x4*>(p);
+      if constexpr (!BF16) b = *reinterpret_cast<const u32x4*>(p + 16);
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if constexpr (BF16)
-        v[i] = __builtin_bit_cast(float, i % 2 ? a[i / 2] & 0xFFFF0000u : a[i / 2] << 16);
-      else
-        v[i] = __builtin_bit_cast(float, i < 4 ? a[i % 4] : b[i % 4]);
-    }
+  } else if (col + 8 <= cols) {
+    __builtin_memcpy(&a, p, 16);
+    if constexpr (!BF16) __builtin_memcpy(&b, p + 16, 16);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -35,29 +32,44 @@ __device__ __forceinline__ void load8(const void* row, int col, int cols, float 
           v[i] = ((const float*)row)[col + i];
       }
     }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if constexpr (BF16)
+      v[i] = __builtin_bit_cast(float, i % 2 ? a[i / 2] & 0xFFFF0000u : a[i / 2] << 16);
+    else
+      v[i] = __builtin_bit_cast(float, i < 4 ? a[i % 4] : b[i % 4]);
   }
 }
 
 template <bool BF16, bool VEC>
 __device__ __forceinline__ void store8(void* row, int col, int cols, const float (&v)[8]) {
-  if constexpr (VEC) {
-    if (col >= cols) return;
-    u32x4* p = reinterpret_cast<u32x4*>((uint8_t*)row + (size_t)col * (BF16 ? 2 : 4));
-    if constexpr (BF16) {
-      p[0] = u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-    } else {
-      *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-      *reinterpret_cast<f32x4*>(p + 1) = f32x4{v[4], v[5], v[6], v[7]};
-    }
-  } else {
+  if (VEC ? col >= cols : col + 8 > cols) {
+    if constexpr (!VEC) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (col + i < cols) {
-        if constexpr (BF16)
-          ((bf16_t*)row)[col + i] = f32_to_bf16(v[i]);
-        else
-          ((float*)row)[col + i] = v[i];
-      }
+      for (int i = 0; i < 8; ++i)
+        if (col + i < cols) {
+          if constexpr (BF16)
+            ((bf16_t*)row)[col + i] = f32_to_bf16(v[i]);
+          else
+            ((float*)row)[col + i] = v[i];
+        }
+    }
+    return;
+  }
+  uint8_t* p = (uint8_t*)row + (size_t)col * (BF16 ? 2 : 4);
+  auto put = [](uint8_t* d, auto x) {
+    if constexpr (VEC)
+      *reinterpret_cast<decltype(x)*>(d) = x;
+    else
+      __builtin_memcpy(d, &x, 16);
+  };
+  if constexpr (BF16) {
+    put(p, u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])});
+  } else {
+    put(p, f32x4{v[0], v[1], v[2], v[3]});
+    put(p + 16, f32x4{v[4], v[5], v[6], v[7]});
   }
 }
 
