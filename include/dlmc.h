@@ -422,6 +422,13 @@ dlmc_status dlmc_token_scores(dlmc_model* model, const void* logits, int32_t dty
 dlmc_status dlmc_token_scores_ws(const dlmc_model* model, int32_t n_rows, int32_t n_top,
                                  uint64_t* ws_bytes);
 
+/* Test hook (host only, no GPU needed): launch number `launch` (from 0) of those that
+ * dlmc_token_scores makes of n_rows rows: its rows (0 past the last launch), the
+ * blocks that each row is split over, and the bytes of ws that it uses, which are
+ * never more than dlmc_token_scores_ws gives for n_rows. */
+dlmc_status dlmc_test_score_launch(int32_t n_rows, int32_t vocab, int32_t n_top, int32_t launch,
+                                   int32_t* rows, int32_t* splits, uint64_t* ws_bytes);
+
 /* Attention-based context scores of one chunk of host tokens[0..T) into
  * host scores[0..T) (two extra forward passes, T <= max_chunk). */
 dlmc_status dlmc_context_scores(dlmc_model* model, const int32_t* tokens, int32_t T, float* scores);

@@ -124,6 +124,7 @@ _SIGS = {
     "dlmc_mx_matmul": (i32, [vp, vp, vp, i32, vp, vp, i32, i32, i32, vp, i32, i64]),
     "dlmc_token_scores": (i32, [vp, vp, i32, i64, i32, vp, i32, vp, vp, vp, vp, vp, u64]),
     "dlmc_token_scores_ws": (i32, [vp, i32, i32, P(u64)]),
+    "dlmc_test_score_launch": (i32, [i32, i32, i32, i32, P(i32), P(i32), P(u64)]),
     "dlmc_status_string": (ctypes.c_char_p, [i32]),
     "dlmc_last_error": (ctypes.c_char_p, []),
 }
@@ -765,6 +766,19 @@ def gemm_tiles(M: int, N: int, K: int, epi: str, d_model: int = 0):
     _check(lib().dlmc_test_gemm_tiles(M, N, K, GEMM_EPI[epi], d_model, ctypes.byref(kind),
                                       ctypes.byref(split)))
     return ("128x128", "192x128", "4wave", "64x64", "128x64", "128x128deep")[kind.value], split.value
+
+
+def score_launches(n_rows: int, vocab: int, top: int):
+    """(rows, splits, workspace bytes) of each launch that token_scores makes of
+    n_rows rows (host only)."""
+    out = []
+    while True:
+        rows, splits, ws = i32(), i32(), u64()
+        _check(lib().dlmc_test_score_launch(n_rows, vocab, top, len(out), ctypes.byref(rows), ctypes.byref(splits),
+                                            ctypes.byref(ws)))
+        if rows.value == 0:
+            return out
+        out.append((rows.value, splits.value, ws.value))
 
 
 def decode_size(data: bytes) -> int:

@@ -569,6 +569,19 @@ dlmc_status dlmc_token_scores(dlmc_model* m, const void* logits, int32_t dtype, 
   });
 }
 
+dlmc_status dlmc_test_score_launch(int32_t n_rows, int32_t vocab, int32_t n_top, int32_t launch, int32_t* rows,
+                                   int32_t* splits, uint64_t* ws_bytes) {
+  return guard([&] {
+    DLMC_CHECK(rows && splits && ws_bytes, DLMC_E_INVAL, "NULL argument");
+    DLMC_CHECK(n_rows >= 0 && vocab >= 2 && n_top >= 0 && n_top <= 64 && n_top <= vocab && launch >= 0, DLMC_E_INVAL,
+               "sizes that token scores do not take");
+    const ScoreLaunch l = score_launch(n_rows, vocab, n_top, launch);
+    *rows = l.rows;
+    *splits = l.splits;
+    *ws_bytes = l.ws;
+  });
+}
+
 dlmc_status dlmc_context_scores(dlmc_model* m, const int32_t* tokens, int32_t T, float* scores) {
   return guard([&] {
     use(m);

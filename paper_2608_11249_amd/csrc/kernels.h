@@ -237,6 +237,15 @@ void mx_matmul(hipStream_t st, MxView A, int fmt_a, size_t a_slots, MxView B, in
 // logits (equal ones by id) with the log2 of their probabilities.  ws: token_scores_ws
 // bytes, needed if that is not 0.
 size_t token_scores_ws(int n_rows, int V, int n_top);
+// Launch i of those that n_rows rows are scored in: its first row, its rows (0 past
+// the last launch), a row to each wave or to one or more blocks (splits), and the
+// bytes of ws that it uses.
+struct ScoreLaunch {
+  size_t first = 0, ws = 0;
+  int rows = 0, splits = 1;
+  bool by_waves = false;
+};
+ScoreLaunch score_launch(int n_rows, int V, int n_top, int i);
 void token_scores(hipStream_t st, const void* logits, bool bf16, size_t ld, int n_rows, int V,
                   const int32_t* tokens, int n_top, float* logp, float* entropy, int32_t* top_ids,
                   float* top_logp, void* ws);

@@ -235,8 +235,6 @@ struct ScoreArgs {
 
 __host__ __device__ inline size_t record_bytes(int k) { return 16 + 16 * (size_t)((k + 1) / 2); }
 
-// A row's results by one wave: its statistics, its token t with logit l, and n >= k entries (one a lane) with
-// the k best among them (n may be less in a row without a distribution).
 // The logit of the row's token; 0 without one within the vocabulary.  (Read ahead of
 // the work that leads up to write_row: two loads one after the other.)
 template <bool BF16>
@@ -247,6 +245,9 @@ __device__ __forceinline__ float token_logit(const ScoreArgs& p, int row, int& t
   return BF16 ? bf16_to_f32(((const bf16_t*)p.logits)[at]) : ((const float*)p.logits)[at];
 }
 
+// A row's results by one wave: its statistics, its token t with logit l, and n >= k
+// entries (one a lane) with the k best among them (n may be less in a row without a
+// distribution).
 __device__ __forceinline__ void write_row(const ScoreArgs& p, int row, Stat s, uint32_t key, uint32_t id, int n, int lane,
                                           int t, float l) {
   // no distribution: nothing above -inf, a NaN, or an infinity
@@ -613,28 +614,8 @@ int splits_of(int n_rows, int V, int n_top) {
   return s < 3 ? 1 : s;
 }
 
-}  // namespace
-
-size_t token_scores_ws(int n_rows, int V, int n_top) {
-  const int s = n_rows > 0 ? splits_of(n_rows, V, n_top) : 1;
-  return s == 1 ? 0 : (size_t)n_rows * s * record_bytes(n_top);
-}
-
-void token_scores(hipStream_t st, const void* logits, bool bf16, size_t ld, int n_rows, int V, const int32_t* tokens,
-                  int n_top, float* logp, float* entropy, int32_t* top_ids, float* top_logp, void* ws) {
-  if (n_rows <= 0) return;
-  DLMC_CHECK(n_top >= 0 && n_top <= MAX_TOP && n_top <= V, DLMC_E_INVAL, "alternatives a row");
-  constexpr int LAUNCH_ROWS = 1 << 23;  // a grid's threads are counted in 32 bits
-  if (n_rows > LAUNCH_ROWS) {           // rows of one block each
-    for (size_t r = 0; r < (size_t)n_rows; r += LAUNCH_ROWS)
-      token_scores(st, (const uint8_t*)logits + r * ld * (bf16 ? 2 : 4), bf16, ld,
-                   (int)std::min<size_t>(n_rows - r, LAUNCH_ROWS), V, tokens ? tokens + r : nullptr, n_top,
-                   tokens ? logp + r : nullptr, entropy + r, n_top ? top_ids + r * n_top : nullptr,
-                   n_top ? top_logp + r * n_top : nullptr, ws);
-    return;
-  }
-  ScoreArgs p{logits, ld, n_rows, V, splits_of(n_rows, V, n_top), n_top, tokens, logp, entropy, top_ids, top_logp, (uint8_t*)ws};
-  const bool wave_rows = rows_by_waves(n_rows, V, n_top);
+void launch_scores(hipStream_t st, bool bf16, bool wave_rows, const ScoreArgs& p) {
+  const int n_rows = p.n_rows, n_top = p.k;
   const unsigned grid = wave_rows ? (unsigned)ceil_div(n_rows, 4) : (unsigned)n_rows * p.splits;
   auto go = [&](auto four, auto one) { (wave_rows ? four : one)<<<grid, 256, 0, st>>>(p); };
   if (n_top == 0)
@@ -650,6 +631,40 @@ void token_scores(hipStream_t st, const void* logits, bool bf16, size_t ld, int 
     if (bf16) scores_join_kernel<true><<<n_rows, 256, 0, st>>>(p);
     else scores_join_kernel<false><<<n_rows, 256, 0, st>>>(p);
     DLMC_HIP(hipGetLastError());
+  }
+}
+
+}  // namespace
+
+// A launch's rows from n_rows in parts of as many as a grid's threads, counted in 32 bits,
+// allow with a block a row.  How a row is taken goes by all rows: a short last part
+// decides nothing for itself, so that no part needs a workspace that the whole does not.
+ScoreLaunch score_launch(int n_rows, int V, int n_top, int i) {
+  constexpr int64_t LAUNCH_ROWS = 1 << 23;
+  const int64_t first = i * LAUNCH_ROWS;
+  ScoreLaunch l{};
+  l.first = (size_t)first;
+  l.rows = (int)std::max<int64_t>(0, std::min(n_rows - first, LAUNCH_ROWS));
+  if (l.rows == 0) return l;
+  l.by_waves = rows_by_waves(n_rows, V, n_top);
+  l.splits = splits_of(n_rows, V, n_top);
+  l.ws = l.splits == 1 ? 0 : (size_t)l.rows * l.splits * record_bytes(n_top);
+  return l;
+}
+
+size_t token_scores_ws(int n_rows, int V, int n_top) { return score_launch(n_rows, V, n_top, 0).ws; }
+
+void token_scores(hipStream_t st, const void* logits, bool bf16, size_t ld, int n_rows, int V, const int32_t* tokens,
+                  int n_top, float* logp, float* entropy, int32_t* top_ids, float* top_logp, void* ws) {
+  DLMC_CHECK(n_top >= 0 && n_top <= MAX_TOP && n_top <= V, DLMC_E_INVAL, "alternatives a row");
+  for (int i = 0;; ++i) {
+    const ScoreLaunch l = score_launch(n_rows, V, n_top, i);
+    if (l.rows == 0) return;
+    const size_t r = l.first;
+    launch_scores(st, bf16, l.by_waves,
+                  ScoreArgs{(const uint8_t*)logits + r * ld * (bf16 ? 2 : 4), ld, l.rows, V, l.splits, n_top,
+                            tokens ? tokens + r : nullptr, tokens ? logp + r : nullptr, entropy + r,
+                            n_top ? top_ids + r * n_top : nullptr, n_top ? top_logp + r * n_top : nullptr, (uint8_t*)ws});
   }
 }
 
