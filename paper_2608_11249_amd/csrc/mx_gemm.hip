@@ -665,6 +665,25 @@ constexpr TileCost TILE_COST[2][TILE_KINDS] = {
 
 }  // namespace
 
+int mx_tiles(int fmt_a, int rows, int N, int K) {
+  const int groups = mx_groups(K);
+  int best = 0;
+  float least = 0.0f;
+  for (int k = 0; k < TILE_KINDS; ++k) {
+    const TileCost& c = TILE_COST[fmt_a == DLMC_MX_FP4 ? 0 : 1][k];
+    // the wide kernels' offsets within a tile are 32 bits wide
+    if (k >= WIDE_128 && groups >= 1 << 13) continue;
+    const float each = std::ceil((float)ceil_div(rows, TILE_ROWS[k]) * (float)ceil_div(N, TILE_COLS[k]) / 256.0f);
+    if (k == WIDE_128_DEEP && fmt_a == DLMC_MX_FP4) continue;  // no faster than with three stages
+    const float us = c.fixed * each + (float)groups * std::max(c.group, each * c.busy);
+    if (k == 0 || us < least) {
+      best = k;
+      least = us;
+    }
+  }
+  return best;
+}
+
 void mx_matmul(hipStream_t st, MxView A, int fmt_a, size_t a_slots, MxView B, int M, int N, int K, const int* M_dev,
                void* out, bool out_bf16, size_t ldo, int rows_hint) {
   if (M <= 0 || N <= 0) return;
@@ -682,21 +701,7 @@ void mx_matmul(hipStream_t st, MxView A, int fmt_a, size_t a_slots, MxView B, in
   p.out = out;
   p.ldo = ldo;
   p.past_caches = (int64_t)M * N * (out_bf16 ? 2 : 4) >= 512ll << 20;  // twice the Infinity Cache
-  const int rows = rows_hint >= 0 && rows_hint < M ? rows_hint : M;
-  int best = 0;
-  float least = 0.0f;
-  for (int k = 0; k < TILE_KINDS; ++k) {
-    const TileCost& c = TILE_COST[fmt_a == DLMC_MX_FP4 ? 0 : 1][k];
-    // the wide kernels' offsets within a tile are 32 bits wide
-    if (k >= WIDE_128 && p.groups >= 1 << 13) continue;
-    const float each = std::ceil((float)ceil_div(rows, TILE_ROWS[k]) * (float)ceil_div(N, TILE_COLS[k]) / 256.0f);
-    if (k == WIDE_128_DEEP && fmt_a == DLMC_MX_FP4) continue;  // no faster than with three stages
-    const float us = c.fixed * each + (float)p.groups * std::max(c.group, each * c.busy);
-    if (k == 0 || us < least) {
-      best = k;
-      least = us;
-    }
-  }
+  const int best = mx_tiles(fmt_a, rows_hint >= 0 && rows_hint < M ? rows_hint : M, N, K);
   if (fmt_a == DLMC_MX_FP4) {
     switch (best) {
       case RING_32x64: return launch_ring<DLMC_MX_FP4, 32, 64, 1, 2, 4, true>(st, p, out_bf16);
