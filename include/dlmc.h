@@ -428,10 +428,12 @@ dlmc_status dlmc_token_scores_ws(const dlmc_model* model, int32_t n_rows, int32_
                                  uint64_t* ws_bytes);
 
 /* Test hook (host only, no GPU needed): the tiles that dlmc_mx_matmul takes for a
- * product of M rows.  *kind: 0 32 x 64, 1 32 x 128, 2 64 x 64, 3 64 x 128, 4 128 x 256, 5
+ * product of M rows (live_rows -1), or a model's head for M rows of which live_rows
+ * are thought to be masked.  *kind: 0 32 x 64, 1 32 x 128, 2 64 x 64, 3 64 x 128, 4 128 x 256, 5
  * 256 x 256, 6 128 x 256 with the whole LDS of a CU (E4M3 only).  The choice never
  * changes a result. */
-dlmc_status dlmc_test_mx_tiles(int32_t fmt_a, int32_t M, int32_t N, int32_t K, int32_t* kind);
+dlmc_status dlmc_test_mx_tiles(int32_t fmt_a, int32_t M, int32_t N, int32_t K, int32_t live_rows,
+                               int32_t* kind);
 
 /* Test hook (host only, no GPU needed): launch number `launch` (from 0) of those that
  * dlmc_token_scores makes of n_rows rows: its rows (0 past the last launch), the

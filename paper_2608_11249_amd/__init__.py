@@ -124,7 +124,7 @@ _SIGS = {
     "dlmc_mx_matmul": (i32, [vp, vp, vp, i32, vp, vp, i32, i32, i32, vp, i32, i64]),
     "dlmc_token_scores": (i32, [vp, vp, i32, i64, i32, vp, i32, vp, vp, vp, vp, vp, u64]),
     "dlmc_token_scores_ws": (i32, [vp, i32, i32, P(u64)]),
-    "dlmc_test_mx_tiles": (i32, [i32, i32, i32, i32, P(i32)]),
+    "dlmc_test_mx_tiles": (i32, [i32, i32, i32, i32, i32, P(i32)]),
     "dlmc_test_score_launch": (i32, [i32, i32, i32, i32, P(i32), P(i32), P(u64)]),
     "dlmc_status_string": (ctypes.c_char_p, [i32]),
     "dlmc_last_error": (ctypes.c_char_p, []),
@@ -773,11 +773,12 @@ def gemm_tiles(M: int, N: int, K: int, epi: str, d_model: int = 0):
 MX_TILES = ("32x64", "32x128", "64x64", "64x128", "128x256", "256x256", "128x256deep")
 
 
-def mx_tiles(fmt: str, M: int, N: int, K: int) -> str:
-    """The tiles that mx_matmul takes of a [M, K] in fmt and b [N, K] (host only);
-    "128x256deep": with the whole LDS of a CU."""
+def mx_tiles(fmt: str, M: int, N: int, K: int, live_rows: int = -1) -> str:
+    """The tiles that mx_matmul takes of a [M, K] in fmt and b [N, K] (host only), or a
+    model's head with so many masked rows of M; "128x256deep": with the whole LDS of
+    a CU."""
     kind = i32()
-    _check(lib().dlmc_test_mx_tiles(MX_FORMAT[fmt], M, N, K, ctypes.byref(kind)))
+    _check(lib().dlmc_test_mx_tiles(MX_FORMAT[fmt], M, N, K, live_rows, ctypes.byref(kind)))
     return MX_TILES[kind.value]
 
 

@@ -569,12 +569,12 @@ dlmc_status dlmc_token_scores(dlmc_model* m, const void* logits, int32_t dtype, 
   });
 }
 
-dlmc_status dlmc_test_mx_tiles(int32_t fmt_a, int32_t M, int32_t N, int32_t K, int32_t* kind) {
+dlmc_status dlmc_test_mx_tiles(int32_t fmt_a, int32_t M, int32_t N, int32_t K, int32_t live_rows, int32_t* kind) {
   return guard([&] {
     DLMC_CHECK(kind, DLMC_E_INVAL, "NULL argument");
     check_mx_shape(fmt_a, M, K);
     DLMC_CHECK(M >= 1 && N >= 1, DLMC_E_INVAL, "no rows");
-    *kind = mx_tiles(fmt_a, M, N, K);
+    *kind = mx_tiles(fmt_a, M, N, K, live_rows);
   });
 }
 

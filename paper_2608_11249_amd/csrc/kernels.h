@@ -230,9 +230,10 @@ void add_norm_mx(hipStream_t st, AddNormMx a);
 // result does not depend on the launch's other rows.
 void mx_matmul(hipStream_t st, MxView A, int fmt_a, size_t a_slots, MxView B, int M, int N, int K,
                const int* M_dev, void* out, bool out_bf16, size_t ldo, int rows_hint = -1);
-// The kind of tile that a product of so many rows takes: 0 32 x 64, 1 32 x 128, 2
+// The kind of tile that such a product takes (M rows, of which rows_hint are thought to
+// be live): 0 32 x 64, 1 32 x 128, 2
 // 64 x 64, 3 64 x 128, 4 128 x 256, 5 256 x 256, 6 128 x 256 with a CU's whole LDS.
-int mx_tiles(int fmt_a, int rows, int N, int K);
+int mx_tiles(int fmt_a, int M, int N, int K, int rows_hint = -1);
 
 // ---------------------------------------------------------------- token scores
 // Of rows of V logits (fp32 or bf16, ld apart): log2 of the probability of

@@ -608,9 +608,7 @@ template <int FA, int TM, int NS, int BLOCKS>
 void launch_wide(hipStream_t st, MxArgs p, bool out_bf16) {
   p.n_tm = ceil_div(p.M, 64 * TM);
   p.n_tn = ceil_div(p.N, 256);
-  const int64_t tiles = (int64_t)p.n_tm * p.n_tn;
-  DLMC_CHECK(tiles < (1ll << 24) - 8, DLMC_E_INVAL, "product with too many tiles");  // threads in 32 bits
-  const unsigned grid = (unsigned)((tiles + 7) & ~7ll);
+  const unsigned grid = (unsigned)(((int64_t)p.n_tm * p.n_tn + 7) & ~7ll);
   if (out_bf16)
     mx_wide_kernel<FA, TM, NS, BLOCKS, true><<<grid, 256, 0, st>>>(p);
   else
@@ -622,9 +620,7 @@ template <int FA, int BM, int BN, int WR, int WC, int NS, bool AHEAD>
 void launch_ring(hipStream_t st, MxArgs p, bool out_bf16) {
   p.n_tm = ceil_div(p.M, BM);
   p.n_tn = ceil_div(p.N, BN);
-  const int64_t tiles = (int64_t)p.n_tm * p.n_tn;
-  DLMC_CHECK(tiles < (1ll << 24) - 8, DLMC_E_INVAL, "product with too many tiles");  // threads in 32 bits
-  const unsigned grid = (unsigned)((tiles + 7) & ~7ll);
+  const unsigned grid = (unsigned)(((int64_t)p.n_tm * p.n_tn + 7) & ~7ll);
   if (out_bf16)
     mx_ring_kernel<FA, BM, BN, WR, WC, NS, AHEAD, true><<<grid, 256, 0, st>>>(p);
   else
@@ -667,22 +663,25 @@ constexpr TileCost TILE_COST[2][TILE_KINDS] = {
 
 }  // namespace
 
-int mx_tiles(int fmt_a, int rows, int N, int K) {
-  const int groups = mx_groups(K);
-  int best = 0;
+int mx_tiles(int fmt_a, int M, int N, int K, int rows_hint) {
+  const int groups = mx_groups(K), rows = rows_hint >= 0 && rows_hint < M ? rows_hint : M;
+  int best = -1;
   float least = 0.0f;
   for (int k = 0; k < TILE_KINDS; ++k) {
     const TileCost& c = TILE_COST[fmt_a == DLMC_MX_FP4 ? 0 : 1][k];
+    // a grid's threads are counted in 32 bits, of all M rows
+    if ((int64_t)ceil_div(M, TILE_ROWS[k]) * ceil_div(N, TILE_COLS[k]) >= (1ll << 24) - 8) continue;
     // the wide kernels' offsets within a tile are 32 bits wide
     if (k >= WIDE_128 && groups >= 1 << 13) continue;
     const float each = std::ceil((float)ceil_div(rows, TILE_ROWS[k]) * (float)ceil_div(N, TILE_COLS[k]) / 256.0f);
     if (k == WIDE_128_DEEP && fmt_a == DLMC_MX_FP4) continue;  // no faster than with three stages
     const float us = c.fixed * each + (float)groups * std::max(c.group, each * c.busy);
-    if (k == 0 || us < least) {
+    if (best < 0 || us < least) {
       best = k;
       least = us;
     }
   }
+  DLMC_CHECK(best >= 0, DLMC_E_INVAL, "product with too many tiles");
   return best;
 }
 
@@ -703,7 +702,7 @@ void mx_matmul(hipStream_t st, MxView A, int fmt_a, size_t a_slots, MxView B, in
   p.out = out;
   p.ldo = ldo;
   p.past_caches = (int64_t)M * N * (out_bf16 ? 2 : 4) >= 512ll << 20;  // twice the Infinity Cache
-  const int best = mx_tiles(fmt_a, rows_hint >= 0 && rows_hint < M ? rows_hint : M, N, K);
+  const int best = mx_tiles(fmt_a, M, N, K, rows_hint);
   if (fmt_a == DLMC_MX_FP4) {
     switch (best) {
       case RING_32x64: return launch_ring<DLMC_MX_FP4, 32, 64, 1, 2, 4, true>(st, p, out_bf16);
