@@ -68,11 +68,16 @@ __device__ __forceinline__ int swizzle(int row) {
   return ROW == 64 ? (row >> 2) & 3 : ROW == 128 ? (row >> 1) & 7 : row & 15;
 }
 
+// Tiles of n rows or columns (unsigned: rounding up may pass 2^31).
+__host__ __device__ inline int tiles_of(int n, int tile) {
+  return (int)(((unsigned)n + (unsigned)tile - 1) / (unsigned)tile);
+}
+
 // This block's tile among those with live rows; hardware block ids go round robin
 // over the 8 XCDs, and each XCD takes a contiguous range of tiles in groups of
 // eight row tiles, which share their operand panels in its L2.
 __device__ __forceinline__ bool tile_of(int bid, int n_tm, int n_tn, int bm, int Mv, int& tm, int& tn) {
-  const int live_m = min(n_tm, (Mv + bm - 1) / bm), live = live_m * n_tn, nb = (live + 7) & ~7;
+  const int live_m = min(n_tm, tiles_of(Mv, bm)), live = live_m * n_tn, nb = (live + 7) & ~7;
   if (bid >= nb) return false;
   const int l = (bid & 7) * (nb >> 3) + (bid >> 3);
   if (l >= live) return false;
@@ -606,8 +611,8 @@ mx_wide_kernel(MxArgs p) {
 
 template <int FA, int TM, int NS, int BLOCKS>
 void launch_wide(hipStream_t st, MxArgs p, bool out_bf16) {
-  p.n_tm = ceil_div(p.M, 64 * TM);
-  p.n_tn = ceil_div(p.N, 256);
+  p.n_tm = tiles_of(p.M, 64 * TM);
+  p.n_tn = tiles_of(p.N, 256);
   const unsigned grid = (unsigned)(((int64_t)p.n_tm * p.n_tn + 7) & ~7ll);
   if (out_bf16)
     mx_wide_kernel<FA, TM, NS, BLOCKS, true><<<grid, 256, 0, st>>>(p);
@@ -618,8 +623,8 @@ void launch_wide(hipStream_t st, MxArgs p, bool out_bf16) {
 
 template <int FA, int BM, int BN, int WR, int WC, int NS, bool AHEAD>
 void launch_ring(hipStream_t st, MxArgs p, bool out_bf16) {
-  p.n_tm = ceil_div(p.M, BM);
-  p.n_tn = ceil_div(p.N, BN);
+  p.n_tm = tiles_of(p.M, BM);
+  p.n_tn = tiles_of(p.N, BN);
   const unsigned grid = (unsigned)(((int64_t)p.n_tm * p.n_tn + 7) & ~7ll);
   if (out_bf16)
     mx_ring_kernel<FA, BM, BN, WR, WC, NS, AHEAD, true><<<grid, 256, 0, st>>>(p);
@@ -670,10 +675,10 @@ int mx_tiles(int fmt_a, int M, int N, int K, int rows_hint) {
   for (int k = 0; k < TILE_KINDS; ++k) {
     const TileCost& c = TILE_COST[fmt_a == DLMC_MX_FP4 ? 0 : 1][k];
     // a grid's threads are counted in 32 bits, of all M rows
-    if ((int64_t)ceil_div(M, TILE_ROWS[k]) * ceil_div(N, TILE_COLS[k]) >= (1ll << 24) - 8) continue;
+    if ((int64_t)tiles_of(M, TILE_ROWS[k]) * tiles_of(N, TILE_COLS[k]) >= (1ll << 24) - 8) continue;
     // the wide kernels' offsets within a tile are 32 bits wide
     if (k >= WIDE_128 && groups >= 1 << 13) continue;
-    const float each = std::ceil((float)ceil_div(rows, TILE_ROWS[k]) * (float)ceil_div(N, TILE_COLS[k]) / 256.0f);
+    const float each = std::ceil((float)tiles_of(rows, TILE_ROWS[k]) * (float)tiles_of(N, TILE_COLS[k]) / 256.0f);
     if (k == WIDE_128_DEEP && fmt_a == DLMC_MX_FP4) continue;  // no faster than with three stages
     const float us = c.fixed * each + (float)groups * std::max(c.group, each * c.busy);
     if (best < 0 || us < least) {

@@ -30,3 +30,13 @@ def test_products_past_every_kind_of_tile_are_refused():
     with pytest.raises(dl.DlmcError) as e:
         dl.mx_tiles("fp8", 1 << 30, 1 << 30, 256)
     assert e.value.code == -1 and "tiles" in str(e.value)
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+@pytest.mark.parametrize("M,N", [(2 ** 31 - 1, 1), (2 ** 31 - 200, 30), (1, 2 ** 31 - 1), (2 ** 31 - 1, 64)])
+def test_sizes_next_to_the_last_int(fmt, M, N):
+    """Rounding up to whole tiles passes 2^31."""
+    bm, bn = map(int, dl.mx_tiles(fmt, M, N, 256).removesuffix("deep").split("x"))
+    assert -(-M // bm) * -(-N // bn) < (1 << 24) - 8
+    small = 2 ** 31 - 300
+    assert dl.mx_tiles(fmt, M, N, 256) == dl.mx_tiles(fmt, min(M, small), min(N, small), 256)
