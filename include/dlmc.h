@@ -345,15 +345,21 @@ dlmc_status dlmc_select_rank_rows(dlmc_model* model, const float* logits, int32_
                                   const int32_t* rank, int32_t* sym);
 /* ---- block-scaled values and token scores (device pointers) -------------- */
 
-/* The calls of this section enqueue their work on the model's stream and return
- * without waiting for it: results are ready once the stream has come that far.
- * They allocate nothing and keep no state between calls, so they may be captured
- * into a HIP graph (dlmc_set_stream to or from a capturing stream is allowed, and
- * does not wait), and calls on several streams do not disturb each other.  They leave the calling thread's
- * current device as it was.  Element types are DLMC_DTYPE_F32 and
- * DLMC_DTYPE_BF16; ld* is the distance of two rows in elements (>= the row's
- * length) and rows need no alignment beyond their elements' own (rows of whole
- * 16-byte chunks are faster). */
+/* The calls of this section enqueue their work on the model's stream, or on their own
+ * if dlmc_set_operator_stream gave them one, and return without waiting for it: results
+ * are ready once the stream has come that far.  They allocate nothing, use no memory of
+ * the model's and keep no state between calls, so they may be captured into a HIP graph,
+ * and what one host thread calls on several streams runs side by side.  They leave the
+ * calling thread's current device as it was.  They compute no gradients.  Element types
+ * are DLMC_DTYPE_F32 and DLMC_DTYPE_BF16; ld* is the distance of two rows in elements
+ * (>= the row's length) and rows need no alignment beyond their elements' own (rows of
+ * whole 16-byte chunks are faster). */
+
+/* Use `hip_stream` (as for dlmc_set_stream, which sets both) for the calls of this
+ * section alone.  Waits for nothing: switching between streams leaves the work on each
+ * running, and either may be under capture.  Results handed from one stream to another
+ * are the caller's to order, as with any work of two streams. */
+dlmc_status dlmc_set_operator_stream(dlmc_model* model, void* hip_stream);
 
 /* Values with block scales: blocks of 32 consecutive columns of a row share a
  * scale 2^(s - 127), one byte, 255 for NaN; the values are E2M1 (+-0, 0.5, 1, 1.5,

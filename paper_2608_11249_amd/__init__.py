@@ -116,6 +116,7 @@ _SIGS = {
     "dlmc_test_head_logits": (i32, [vp, i32]),
     "dlmc_test_gemm_tiles": (i32, [i32, i32, i32, i32, i32, ctypes.POINTER(ctypes.c_int32),
                                    ctypes.POINTER(ctypes.c_int32)]),
+    "dlmc_set_operator_stream": (i32, [vp, vp]),
     "dlmc_mx_bytes": (i32, [i32, i32, i32, P(u64), P(u64)]),
     "dlmc_mx_quantize": (i32, [vp, vp, i32, i64, i32, i32, i32, vp, vp]),
     "dlmc_mx_dequantize": (i32, [vp, vp, vp, i32, i32, i32, vp, i32, i64]),
@@ -345,6 +346,7 @@ class Model:
         self._trace_cb = None
         self._ws_sizes = {}
         self._stream = None  # what set_stream was last given
+        self._op_stream = None  # the stream of the calls that return without waiting
         self._hook_stream = False  # whether that was a stage hook's default stream
 
     def close(self):
@@ -468,7 +470,7 @@ class Model:
 
     def set_stream(self, stream_handle: Optional[int]):
         _check(lib().dlmc_set_stream(self.handle, stream_handle))
-        self._stream = stream_handle or None
+        self._stream = self._op_stream = stream_handle or None
         self._hook_stream = False
 
     def _off_default_stream(self):
@@ -483,14 +485,11 @@ class Model:
         fills its tensors (which live until it returns).  The default stream's
         handle is 0, for which the library would take its own stream."""
         import torch
-        self._follow(torch.cuda.current_stream(device).cuda_stream)
-        _check(fn(self.handle, *(_ptr(a) if torch.is_tensor(a) else a for a in args)))
-
-    def _follow(self, handle: int):
-        stream = handle or DEFAULT_STREAM
-        if stream != self._stream:
+        stream = torch.cuda.current_stream(device).cuda_stream or DEFAULT_STREAM
+        if stream != self._stream or stream != self._op_stream:
             self.set_stream(stream)
             self._hook_stream = stream == DEFAULT_STREAM
+        _check(fn(self.handle, *(_ptr(a) if torch.is_tensor(a) else a for a in args)))
 
     def forward_logits(self, state):
         """state: int32 cuda tensor [B, T].  Returns (logits [n, V], rows [n])."""
@@ -580,10 +579,14 @@ class Model:
         return sel_pos, sel_row, n_sel
 
     # ---- block-scaled values and token scores (torch device tensors; the calls
-    # return without waiting for the GPU, so what they cost a short launch is the
-    # host's time: one pass of checks, no copies, raw pointers)
+    # return without waiting for the GPU, nor for other streams when the current one
+    # changes, so what they cost a short launch is the host's time: one pass of checks, no
+    # copies, raw pointers)
     def _call(self, fn, *args):
-        self._follow(_raw_stream(self.device))
+        stream = _raw_stream(self.device) or DEFAULT_STREAM
+        if stream != self._op_stream:
+            _check(lib().dlmc_set_operator_stream(self.handle, stream))
+            self._op_stream = stream
         st = fn(self.handle, *args)
         if st:
             _check(st)

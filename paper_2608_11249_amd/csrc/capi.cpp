@@ -64,6 +64,10 @@ bool capturing(hipStream_t s) {
   return now != hipStreamCaptureStatusNone;
 }
 
+hipStream_t stream_of(const dlmc_model* m, void* hip_stream) {
+  return hip_stream == DLMC_DEFAULT_STREAM ? nullptr : hip_stream ? (hipStream_t)hip_stream : m->own_stream;
+}
+
 bool is_bf16(int32_t dtype) {
   DLMC_CHECK(dtype == DLMC_DTYPE_F32 || dtype == DLMC_DTYPE_BF16, DLMC_E_INVAL, "element type must be fp32 or bf16");
   return dtype == DLMC_DTYPE_BF16;
@@ -122,13 +126,18 @@ void dlmc_model_destroy(dlmc_model* model) { delete model; }
 dlmc_status dlmc_set_stream(dlmc_model* m, void* hip_stream) {
   return guard([&] {
     OnDevice on(m);
-    hipStream_t const next = hip_stream == DLMC_DEFAULT_STREAM ? nullptr
-                             : hip_stream                       ? (hipStream_t)hip_stream
-                                                                : m->own_stream;
+    hipStream_t const next = stream_of(m, hip_stream);
     // no wait in a capture, which it would end: a call that uses the model's buffers
     // has waited for its work itself
     if (!capturing(next) && !capturing(m->stream)) DLMC_HIP(hipStreamSynchronize(m->stream));
-    m->stream = next;
+    m->stream = m->op_stream = next;
+  });
+}
+
+dlmc_status dlmc_set_operator_stream(dlmc_model* m, void* hip_stream) {
+  return guard([&] {
+    DLMC_CHECK(m, DLMC_E_INVAL, "model is NULL");
+    m->op_stream = stream_of(m, hip_stream);
   });
 }
 
@@ -469,7 +478,7 @@ dlmc_status dlmc_mx_quantize(dlmc_model* m, const void* x, int32_t dtype, int64_
     check_mx_shape(fmt, rows, cols);
     if (rows == 0) return;
     check_rows(x, ldx, cols, bf16 ? 2 : 4, "x");
-    mx_quantize(m->stream, x, bf16, (size_t)ldx, rows, cols, fmt, mx_view(codes, scales));
+    mx_quantize(m->op_stream, x, bf16, (size_t)ldx, rows, cols, fmt, mx_view(codes, scales));
   });
 }
 
@@ -481,7 +490,7 @@ dlmc_status dlmc_mx_dequantize(dlmc_model* m, const uint8_t* codes, const uint8_
     check_mx_shape(fmt, rows, cols);
     if (rows == 0) return;
     check_rows(out, ldo, cols, bf16 ? 2 : 4, "out");
-    mx_dequantize(m->stream, mx_view(codes, scales), fmt, rows, cols, out, bf16, (size_t)ldo);
+    mx_dequantize(m->op_stream, mx_view(codes, scales), fmt, rows, cols, out, bf16, (size_t)ldo);
   });
 }
 
@@ -519,7 +528,7 @@ dlmc_status dlmc_add_norm_mx(dlmc_model* m, const void* x, int32_t dtype, int64_
     a.norm_kind = norm_kind;
     a.fmt = fmt;
     a.eps = eps;
-    add_norm_mx(m->stream, a);
+    add_norm_mx(m->op_stream, a);
   });
 }
 
@@ -534,7 +543,7 @@ dlmc_status dlmc_mx_matmul(dlmc_model* m, const uint8_t* a_codes, const uint8_t*
     if (M == 0 || N == 0) return;
     const MxView a = mx_view(a_codes, a_scales), b = mx_view(b_codes, b_scales);
     check_rows(out, ldo, N, bf16 ? 2 : 4, "out");
-    mx_matmul(m->stream, a, fmt_a, mx_slots(M), b, M, N, K, nullptr, out, bf16, (size_t)ldo);
+    mx_matmul(m->op_stream, a, fmt_a, mx_slots(M), b, M, N, K, nullptr, out, bf16, (size_t)ldo);
   });
 }
 
@@ -564,7 +573,7 @@ dlmc_status dlmc_token_scores(dlmc_model* m, const void* logits, int32_t dtype, 
     const uint64_t need = token_scores_ws(n_rows, V, n_top);
     DLMC_CHECK(need == 0 || (ws && ((uintptr_t)ws & 15) == 0 && ws_bytes >= need), DLMC_E_INVAL,
                "the workspace needs " + std::to_string(need) + " bytes, 16-byte aligned");
-    token_scores(m->stream, logits, bf16, (size_t)ld, n_rows, V, tokens, n_top, logp_bits, entropy_bits, top_ids,
+    token_scores(m->op_stream, logits, bf16, (size_t)ld, n_rows, V, tokens, n_top, logp_bits, entropy_bits, top_ids,
                  top_logp_bits, ws);
   });
 }

@@ -216,7 +216,7 @@ void create_model(dlmc_model* m, const dlmc_model_config& cfg, uint64_t seed, in
   DLMC_HIP(hipSetDevice(device));
   m->scratch = scratch_address(device);  // looked up once per device, with it current
   DLMC_HIP(hipStreamCreateWithFlags(&m->own_stream, hipStreamNonBlocking));
-  m->stream = m->own_stream;
+  m->stream = m->op_stream = m->own_stream;
   m->cfg = cfg;
   m->seed = seed;
   m->bf16 = cfg.dtype != DLMC_DTYPE_F32;

@@ -14,6 +14,7 @@ struct dlmc_model {
   uint64_t seed = 0;
   int device = 0;
   hipStream_t stream = nullptr;      // stream in use
+  hipStream_t op_stream = nullptr;   // of the calls that use no memory of the model's
   hipStream_t own_stream = nullptr;  // library-created stream
   size_t esz = 2;                    // bytes per weight / GEMM-input element
   bool bf16 = true;
