@@ -581,7 +581,8 @@ class Model:
     # ---- block-scaled values and token scores (torch device tensors; the calls
     # return without waiting for the GPU, nor for other streams when the current one
     # changes, so what they cost a short launch is the host's time: one pass of checks, no
-    # copies, raw pointers)
+    # copies, raw pointers.  They compute no gradients: what they compute requires none,
+    # whatever the inputs do, and an `out` that does is refused, but under torch.no_grad())
     def _call(self, fn, *args):
         stream = _raw_stream(self.device) or DEFAULT_STREAM
         if stream != self._op_stream:
@@ -616,6 +617,18 @@ class Model:
         elif ld < c:
             _refuse(f"{what}: rows overlap")
         return code, ld, t.data_ptr()
+
+    def _out(self, t, cols: int):
+        """As _rows, of a tensor that is to be written."""
+        if getattr(t, "requires_grad", False) and _torch().is_grad_enabled():
+            _refuse("out requires a gradient, and these calls compute none")
+        return self._rows(t, "out", cols)
+
+    @staticmethod
+    def _wrote(t):
+        """Lets autograd see that t has other values (a graph that saved them refuses to
+        go on)."""
+        _torch().autograd.graph.increment_version(t)
 
     def _vector(self, t, what: str, n: int, dtype):
         if getattr(t, "dtype", None) != dtype or t.dim() != 1 or t.shape[0] != n:
@@ -679,7 +692,7 @@ class Model:
             gptr = gain.data_ptr()
         if out is not None:
             r = out
-            ocode, lds, sptr = self._rows(out, "out", cols)
+            ocode, lds, sptr = self._out(out, cols)
             if ocode != code or out.shape[0] != rows:
                 _refuse("out must have x's shape and type")
         elif delta is None:
@@ -691,6 +704,8 @@ class Model:
         self._call(lib().dlmc_add_norm_mx, ptr, code, ld, dptr, dcode, ldd, sptr, lds, gptr, kind,
                    self.shape.norm_eps if eps is None else eps, rows, cols, MX_FORMAT[fmt],
                    *q._ptrs)
+        if out is not None:
+            self._wrote(out)
         return r, q
 
     def mx_matmul(self, a: MXMatrix, b: MXMatrix, out_dtype=None, out=None):
@@ -704,16 +719,19 @@ class Model:
         M, N, K = a.rows, b.rows, a.cols
         if K != b.cols:
             _refuse(f"a has {K} columns, b {b.cols}")
-        if out is None:
+        given = out is not None
+        if not given:
             dtype = _torch().float32 if out_dtype is None else out_dtype
             code, ldo = self._out_type(dtype), N
             out = a._new(dtype, M, N)
             optr = out.data_ptr()
         else:
-            code, ldo, optr = self._rows(out, "out", N)
+            code, ldo, optr = self._out(out, N)
             if out.shape[0] != M or (out_dtype is not None and out.dtype != out_dtype):
                 _refuse("out does not have the product's shape and type")
         self._call(lib().dlmc_mx_matmul, ac, asc, MX_FORMAT[a.fmt], bc, bsc, M, N, K, optr, code, ldo)
+        if given:
+            self._wrote(out)
         return out
 
     def _scores_ws(self, n: int, top: int) -> int:
