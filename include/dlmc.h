@@ -392,8 +392,8 @@ dlmc_status dlmc_mx_dequantize(dlmc_model* model, const uint8_t* codes, const ui
                                int64_t ldo);
 /* Pre-norm of a residual stream with its branch's addition: r = x + delta (x
  * alone if delta is NULL), rounded to x's type and stored in sum[rows, cols] (of
- * x's type; may be x itself; NULL: not stored; x, delta and sum must not overlap
- * otherwise), then y = r / sqrt(mean(r^2) + eps) (DLMC_NORM_RMS) or (r - mean(r)) /
+ * x's type; may be x itself, or a delta of x's type; NULL: not stored; a sum that
+ * overlaps x or delta otherwise is refused), then y = r / sqrt(mean(r^2) + eps) (DLMC_NORM_RMS) or (r - mean(r)) /
  * sqrt(var(r) + eps) (DLMC_NORM_LAYER), times gain[cols] (fp32; NULL: 1),
  * quantised as by dlmc_mx_quantize.  All arithmetic is in fp32; a row's result
  * does not depend on the others.  cols <= 8192. */

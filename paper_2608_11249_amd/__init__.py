@@ -672,7 +672,7 @@ class Model:
     def add_norm_mx(self, x, delta=None, gain=None, fmt: str = "fp8", norm: Optional[str] = None,
                     eps: Optional[float] = None, out=None):
         """(r, q): r = x + delta [rows, cols] in x's type (x itself without a delta;
-        written to `out`, which may be x, if given) and its norm times gain (fp32)
+        written to `out`, which may be x or delta, if given) and its norm times gain (fp32)
         as an MXMatrix.  norm ("rmsnorm" or "layernorm") and eps: the model's."""
         code, ld, ptr = self._rows(x, "x")
         rows, cols = x.shape

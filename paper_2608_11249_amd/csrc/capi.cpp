@@ -78,6 +78,16 @@ void check_rows(const void* p, int64_t ld, int32_t n, int bytes, const char* wha
   DLMC_CHECK((uintptr_t)p % bytes == 0, DLMC_E_INVAL, std::string(what) + " is not aligned to its elements");
   DLMC_CHECK(ld >= n, DLMC_E_INVAL, std::string(what) + ": rows overlap");
 }
+// Whether rows x cols elements of p and of q share memory (of rows at different
+// distances: whether the ranges that they span do).
+bool share(const void* p, int64_t ldp, int esp, const void* q, int64_t ldq, int esq, int32_t rows, int32_t cols) {
+  const uint64_t a = (uintptr_t)p, b = (uintptr_t)q, pa = ldp * esp, pb = ldq * esq, wa = (uint64_t)cols * esp,
+                 wb = (uint64_t)cols * esq;
+  if (a + (rows - 1) * pa + wa <= b || b + (rows - 1) * pb + wb <= a) return false;
+  if (pa != pb) return true;
+  const uint64_t d = b >= a ? (b - a) % pa : (pa - (a - b) % pa) % pa;  // b's columns behind a's
+  return d < wa || pa - d < wb;
+}
 void check_mx_shape(int32_t fmt, int32_t rows, int32_t cols) {
   DLMC_CHECK(fmt == DLMC_MX_FP4 || fmt == DLMC_MX_FP8, DLMC_E_INVAL, "no such block-scaled format");
   DLMC_CHECK(rows >= 0, DLMC_E_INVAL, "negative number of rows");
@@ -512,7 +522,11 @@ dlmc_status dlmc_add_norm_mx(dlmc_model* m, const void* x, int32_t dtype, int64_
     check_rows(x, ldx, cols, es, "x");
     if (delta) check_rows(delta, ldd, cols, a.delta_bf16 ? 2 : 4, "delta");
     if (sum) check_rows(sum, lds, cols, es, "sum");
-    DLMC_CHECK(sum != x || lds == ldx, DLMC_E_INVAL, "a sum stored in x has x's rows");
+    if (sum && !(sum == x && lds == ldx))
+      DLMC_CHECK(!share(sum, lds, es, x, ldx, es, rows, cols), DLMC_E_INVAL, "sum overlaps x, but is not x");
+    if (sum && delta && !(sum == delta && lds == ldd && a.delta_bf16 == a.x_bf16))
+      DLMC_CHECK(!share(sum, lds, es, delta, ldd, a.delta_bf16 ? 2 : 4, rows, cols), DLMC_E_INVAL,
+                 "sum overlaps delta, but is not delta");
     DLMC_CHECK((uintptr_t)gain % 4 == 0, DLMC_E_INVAL, "gain is not aligned to its elements");
     a.q = mx_view(codes, scales);
     a.x = x;
