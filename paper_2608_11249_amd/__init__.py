@@ -24,6 +24,7 @@ FFN = {"gelu": 0, "swiglu": 1}
 NORM = {"layernorm": 0, "rmsnorm": 1}
 DTYPE = {"f32": 0, "bf16": 1, "bf16-mx4head": 2}  # bf16-mx4head: the LM head in E2M1
 MX_FORMAT = {"fp4": 0, "fp8": 1}  # E2M1, E4M3
+MAX_ROWS = 2 ** 31 - 1  # of a matrix that a call takes
 FLAG_CRC = 1
 STAGES = ["embed", "norm", "qkv", "attn", "oproj", "ffn_in", "ffn_out", "head", "entropy",
           "select", "cdf", "reveal", "compact"]
@@ -194,7 +195,7 @@ class MXMatrix:
     def _shapes(fmt: str, rows: int, cols: int):
         if fmt not in MX_FORMAT:
             _refuse(f"format must be fp4 or fp8, not {fmt!r}")
-        if rows < 0 or not 1 <= cols <= 1 << 24:
+        if not 0 <= rows <= MAX_ROWS or not 1 <= cols <= 1 << 24:
             _refuse(f"no matrix of {rows} x {cols} values is held")
         groups = (cols + 255) >> 8
         return (rows, groups << (7 if fmt == "fp4" else 8)), (groups, (rows + 31) & -32, 8)
@@ -607,6 +608,8 @@ class Model:
         if t.get_device() != self.device:
             self._here(t, what)
         n, c = t.shape
+        if n > MAX_ROWS:
+            _refuse(f"{what} has more rows than {MAX_ROWS}")
         if cols is not None and c != cols:
             _refuse(f"{what} must have {cols} columns, not {c}")
         ld, step = t.stride()
