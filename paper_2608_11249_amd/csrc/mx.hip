@@ -90,9 +90,10 @@ __device__ __forceinline__ void put8(uint8_t* codes, size_t pitch, uint8_t* scal
 
 // Groups of columns that a block of mx_quantize / mx_dequantize takes of each of
 // its eight rows (32 lanes to a group, eight columns a lane).  HBM bound: 32768 x 4096
-// from bf16 to E2M1 61 us, 5.6 TB/s, and back to bf16 59 us.  The blocks of a row follow
-// each other, so that what is in flight lies together in memory (rows first: 73 and
-// 73); four groups a block take 64 and 59.
+// from bf16 to E2M1 62 us, 5.6 TB/s, and back to bf16 58 us, each alone (in turn 77 and
+// 49, as the caches hold the other's data).  The blocks of a row follow each other, so
+// that what is in flight lies together in memory (rows first: 73 and 73, each alone);
+// four groups a block take 64 and 59.
 constexpr int Q_GROUPS = 2;
 
 template <int FMT, bool BF16, bool VEC>
@@ -157,7 +158,7 @@ __device__ __forceinline__ float wave_total(float t) {
 // columns alone, so its sums, and with them its codes, do not depend on the
 // number of rows.  HBM bound: x and delta are read once, and everything is in
 // flight before the first value is used (2048 x 4096 in fp32 with a bf16 delta, to E4M3:
-// 17.5 us, 5.3 TB/s).
+// 17.6 us, 5.3 TB/s).
 template <int FMT, bool XB, bool VEC, int WAVES, int PER>
 __global__ void __launch_bounds__(256)
 add_norm_mx_kernel(AddNormMx a) {

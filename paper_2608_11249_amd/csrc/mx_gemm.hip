@@ -107,7 +107,7 @@ struct MxArgs {
 // AHEAD: for launches that leave a CU one tile, where nothing but the wave's own
 // instructions hides a latency: a group's fragments are read into registers under the
 // products of the group before, and loads and reads are issued between the products,
-// each of which waits for the one before (1 x 4096 x 4096 in E2M1 8.5 -> 6.1 us then).
+// each of which waits for the one before (1 x 4096 x 4096 in E2M1 8.5 -> 6.1 us).
 // Without it a CU takes two to four blocks, which hide each other's waits, and the
 // registers of a second set of fragments would cost blocks (2048 x 4096 x 4096 in E4M3
 // on 64 x 128 tiles 36 us, with it 52).
@@ -650,12 +650,10 @@ void launch_ring(hipStream_t st, MxArgs p, bool out_bf16) {
 // a tile beside its groups (start, epilogue), of a group of 256 columns where a CU has
 // one tile, and of a group per tile where it has more (`busy`: the tiles of a CU
 // share the filling and reading of its LDS); the CU with the most tiles counts.
-// Measured at 1 .. 8192 rows, 768 .. 12288 columns and widths of 2304 .. 126464,
-// launches of one kernel each; over a hundred sizes the choice takes 2.5% longer than
-// the fastest kernel on average, a fifth at most.  Some of what they come from, in us
-// (E2M1 / E4M3):
+// Fitted to times at 1 .. 8192 rows, 768 .. 12288 columns and widths of 2304 .. 126464,
+// launches of one kernel each, among them, in us (E2M1 / E4M3):
 //   rows x width x columns    32x64       32x128      64x64       64x128      128x256     256x256
-//       1 x   4096 x  4096    6.1 / 6.8   8.5 / 9.9   7.2 / 8.4    10 / 11     16 / 23     25 / 37
+//       1 x   4096 x  4096    6.0 / 6.7   8.5 / 9.9   7.2 / 8.4    10 / 11     16 / 23     25 / 37
 //      16 x 126464 x  4096     40 / 44     40 / 40     43 / 54     47 / 44     46 / 61     64 / 93
 //     128 x  12288 x  4096     12 / 16     11 / 12    9.7 / 11     12 / 14     17 / 31     26 / 39
 //     777 x   4099 x  1000     11 / 16    9.3 / 10    6.9 / 8.9   7.3 / 8.2    13 / 16     23 / 26
