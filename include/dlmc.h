@@ -165,7 +165,8 @@ void dlmc_model_destroy(dlmc_model* model);
  * DLMC_DEFAULT_STREAM selects the device's default stream (handle 0, e.g. torch's
  * unless another is current), and NULL the library's own stream, which waits
  * for no other: device memory handed to a call on it has to be ready.  Waits for
- * the work on the stream used before, unless one of the two is being captured. */
+ * the work on the stream used before (not on one that dlmc_set_operator_stream gave),
+ * unless one of the two is being captured. */
 #define DLMC_DEFAULT_STREAM ((void*)1)
 dlmc_status dlmc_set_stream(dlmc_model* model, void* hip_stream);
 
@@ -280,8 +281,8 @@ dlmc_status dlmc_test_inject_nonfinite(dlmc_model* model, int32_t on);
  * models).  With many masked rows, the head writes only each row's entropy
  * statistics (Schedules, item 3) and the logits of the rows committed in the
  * pass are computed after the selection, which gives the same bits as storing
- * them all (a head in E2M1 always stores them).  mode 0 (default): decided per pass by estimated cost; 1: always
- * deferred; 2: never.  Payloads do not depend on the mode.  E_INVAL for
+ * them all (a head in E2M1 always stores them).  mode 0 (default): decided per
+ * pass by estimated cost; 1: always deferred; 2: never.  Payloads do not depend on the mode.  E_INVAL for
  * another mode. */
 dlmc_status dlmc_test_head_logits(dlmc_model* model, int32_t mode);
 
